@@ -346,6 +346,143 @@ sparsepr_status sparsepr_get_timings(sparsepr_plan_t plan, sparsepr_timings* out
 /* Release the handle (not the workspace).  NULL is ignored. */
 void sparsepr_plan_destroy(sparsepr_plan_t plan);
 
+/* ---- operators on a K/V cache ---------------------------------------------
+ *
+ * For models that generate token by token or frame by frame: keys and values
+ * of the past stay in a cache of a fixed number of slots, new tokens attend to
+ * it, and the slots that matter least make room.  One step is
+ *   sparsepr_cache_attend      the new tokens (one, a drafted tree or a frame)
+ *                              attend to the cache and to each other;
+ *   sparsepr_cache_append      the accepted ones of them enter the cache;
+ *   sparsepr_cache_accumulate  the weights that they gave the slots are added
+ *                              to the slots' scores;
+ *   sparsepr_cache_evict       the slots of the least score leave.
+ *
+ * A cache is caller memory: this struct holds its geometry and DEVICE pointers
+ * and is read on the host during the call.  Slots 0 .. lengths[b] - 1 of batch
+ * entry b are in use, the same number in each K/V head (which slots are kept
+ * differs by head); what the other slots hold is never used, NaN included.
+ * lengths are read on the device (clamped to [0, capacity]), so the calls can
+ * be captured into a graph and replayed as the cache grows.  Attention does
+ * not depend on the order of the slots; after an eviction it is not the order
+ * of time, which `positions` keeps.  Strides count elements; the last
+ * dimension of K and V is contiguous.  No output of a call may overlap one of
+ * its inputs except where that is said. */
+typedef struct {
+  int32_t batch, heads_kv, capacity, d;  /* d in {64, 128} */
+  int64_t stride_b, stride_h, stride_n;  /* k and v: [batch, heads_kv, capacity, d] */
+  int32_t dtype;                         /* sparsepr_dtype of k, v and of the call's tensors */
+  void* k;
+  void* v;
+  int32_t* lengths;    /* [batch] slots in use */
+  float* scores;       /* [batch, heads_kv, capacity] contiguous: accumulated attention
+                          weight of each slot; may be NULL where a call does not need it */
+  int32_t* positions;  /* [batch, heads_kv, capacity] contiguous: token position (>= 0) of
+                          each slot; may be NULL where a call does not need it */
+  int32_t* flags;      /* [batch] or NULL: SPARSEPR_CACHE_FLAG_* found on the device are
+                          OR-ed in; the caller clears them */
+} sparsepr_cache;
+
+#define SPARSEPR_CACHE_FLAG_OVERFLOW 1  /* append: the rows do not fit; none was appended */
+#define SPARSEPR_CACHE_FLAG_BAD_INDEX 2 /* append: a row index outside [0, n): none was appended;
+                                           accumulate: such rows were left out; attend: a parent
+                                           outside [-1, own index): the token was taken for a root */
+
+/* How the new tokens see each other (all of them see the whole cache). */
+#define SPARSEPR_TOKENS_CAUSAL 0 /* token t sees the tokens 0 .. t */
+#define SPARSEPR_TOKENS_FULL 1   /* every token sees every one of them */
+#define SPARSEPR_TOKENS_TREE 2   /* token t sees itself and its ancestors; n <= 256 */
+
+/* The new tokens of a call: Q and the output [batch, heads, n, d], their K and V
+ * [batch, heads_kv, n, d], of the cache's dtype.  heads is a multiple of the
+ * cache's heads_kv: query heads h*G .. h*G + G-1 attend to K/V head h. */
+typedef struct {
+  int32_t heads, n;
+  int64_t stride_b, stride_h, stride_n;          /* Q */
+  int64_t out_stride_b, out_stride_h, out_stride_n; /* the output; rows must not overlap */
+  int64_t kv_stride_b, kv_stride_h, kv_stride_n; /* new K and V */
+  int32_t mask;                                  /* SPARSEPR_TOKENS_* */
+} sparsepr_tokens;
+
+/* Attention of the new tokens over the cache and themselves:
+ *   out = softmax(q [K_cache; K_new]^T / sqrt(d)) [V_cache; V_new]
+ * over the slots in use and the new tokens that `mask` lets a token see.
+ *   parents  [batch, n], for TREE (else NULL): parents[t] < t is the token that
+ *            t continues, -1 if it continues the cache.
+ *   counts   [batch] or NULL (= n): tokens of each entry, clamped to [0, n].  Rows
+ *            of out and lse behind them are left as they were, and what K_new and
+ *            V_new hold there is never used; nor does a K or V row reach a token
+ *            that does not see it, whatever it holds.
+ *   lse      [batch, heads, n] contiguous or NULL: log sum exp of each row's scores
+ *            (natural logarithm), which sparsepr_cache_accumulate takes.
+ * Sums are in float32; with bf16 inputs the weights of the V product are
+ * rounded to bf16, lse is not.  `workspace` (16-byte aligned) holds
+ * sparsepr_cache_attend_workspace_size bytes (which depend on the geometry
+ * alone) and belongs to the call until its work has completed.
+ * Errors (all four operators): INVALID_ARGUMENT for bad pointers, sizes and
+ * ranges; UNSUPPORTED for d not in {64, 128}, rows of K, V, Q or the output
+ * (base pointers and strides) not 16-byte aligned, n * heads / heads_kv or capacity above 2^28,
+ * batch * heads_kv above 65535, a tree of more than 256 tokens. */
+sparsepr_status sparsepr_cache_attend_workspace_size(const sparsepr_cache* cache,
+                                                     const sparsepr_tokens* tokens, size_t* bytes);
+sparsepr_status sparsepr_cache_attend(const sparsepr_cache* cache, const sparsepr_tokens* tokens,
+                                      const void* q, const void* k_new, const void* v_new,
+                                      const int32_t* parents, const int32_t* counts, void* out,
+                                      float* lse, void* workspace, size_t bytes, void* stream);
+
+/* Append rows of new K and V behind the slots in use: slot lengths[b] + i of entry b
+ * takes new token rows[b, i], i < counts[b].  Their scores become 0 and their
+ * positions those of the tokens (each where the cache has the array).
+ *   token_positions [batch, n]: required exactly when the cache has positions.
+ *   rows         [batch, n_rows] token indices (an accepted path, say), or NULL:
+ *                the tokens in order (n_rows = n).
+ *   counts       [batch] or NULL (= n_rows), clamped to [0, n_rows].
+ *   lengths_out  [batch]: the new lengths; may be cache->lengths itself.
+ * An entry whose rows do not fit or whose list has an index outside [0, n) is
+ * left as it is, its flag set.  Needs no workspace. */
+sparsepr_status sparsepr_cache_append(const sparsepr_cache* cache, const sparsepr_tokens* tokens,
+                                      const void* k_new, const void* v_new,
+                                      const int32_t* token_positions, const int32_t* rows,
+                                      int32_t n_rows, const int32_t* counts, int32_t* lengths_out,
+                                      void* stream);
+
+/* Add the attention weights of rows that were just appended to the scores of the
+ * slots they saw: with L = lengths[b] and c = counts[b] (both after the append of
+ * the same rows), row i is token rows[b, i], sits in slot L - c + i and gives
+ *   scores[b, h, j] += sum over its query heads of exp(q k_j / sqrt(d) - lse)
+ * to the slots j <= L - c + i (CAUSAL and TREE) or j < L (FULL).  q and lse are
+ * those of the attend call.  To weigh by the last tokens of a prompt only, pass
+ * these alone.  Each slot's sum is taken in a fixed order: the same inputs give
+ * the same scores.  Rows whose lse is -inf add nothing. */
+sparsepr_status sparsepr_cache_accumulate_workspace_size(const sparsepr_cache* cache,
+                                                         const sparsepr_tokens* tokens,
+                                                         int32_t n_rows, size_t* bytes);
+sparsepr_status sparsepr_cache_accumulate(const sparsepr_cache* cache,
+                                          const sparsepr_tokens* tokens, const void* q,
+                                          const float* lse, const int32_t* rows, int32_t n_rows,
+                                          const int32_t* counts, void* workspace, size_t bytes,
+                                          void* stream);
+
+/* Keep at most `budget` slots of every K/V head: the slots of positions below
+ * n_sink, those of the n_recent newest positions (position > newest - n_recent),
+ * and of the others those of the largest scores; equal ranks go to the lowest
+ * slot, and a NaN score ranks above every number.  Kept slots below `budget` stay
+ * where they are; the others move, in ascending order, into the slots below
+ * `budget` that became free (K, V, score and position), so that few rows move.
+ * Entries of at most `budget` slots keep all.
+ *   to      NULL: in place (budget <= capacity), lengths become min(length, budget).
+ *           Else another cache of the same batch, heads_kv, d and dtype and of at
+ *           least `budget` slots: every kept row is copied to the same slot of it as
+ *           above, `cache` is left as it is and to->lengths are written.
+ * cache->scores is required, positions where n_sink or n_recent is not 0;
+ * n_sink + n_recent <= budget.  Scores and positions move where both caches have
+ * them. */
+sparsepr_status sparsepr_cache_evict_workspace_size(const sparsepr_cache* cache, int32_t budget,
+                                                    size_t* bytes);
+sparsepr_status sparsepr_cache_evict(const sparsepr_cache* cache, const sparsepr_cache* to,
+                                     int32_t budget, int32_t n_sink, int32_t n_recent,
+                                     void* workspace, size_t bytes, void* stream);
+
 /* Text of the calling thread's most recent failure ("" if none); valid until
  * that thread's next call into the library. */
 const char* sparsepr_last_error(void);

@@ -13,7 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsparsepr.so")
-SOURCES = ["plan_kernels.hip", "attn_kernels.hip", "fit_kernels.hip", "noalloc.hip", "api.cpp"]
+SOURCES = ["plan_kernels.hip", "attn_kernels.hip", "fit_kernels.hip", "cache_kernels.hip",
+           "noalloc.hip", "api.cpp", "cache_api.cpp"]
 ARCH = os.environ.get("SPARSEPR_OFFLOAD_ARCH", "gfx950")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -52,9 +53,9 @@ def build(verbose: bool = False) -> str:
 
 
 # Host-side sanitizer build: api.cpp (argument validation, workspace layout,
-# export/import, timing) holds no device code, so g++ compiles it with
-# AddressSanitizer and UndefinedBehaviorSanitizer and it is linked with the
-# regular kernel objects into libsparsepr_san.so.  The binding loads it when
+# export/import, timing) and cache_api.cpp hold no device code, so g++ compiles
+# them with AddressSanitizer and UndefinedBehaviorSanitizer and they are linked
+# with the regular kernel objects into libsparsepr_san.so.  The binding loads it when
 # SPARSEPR_LIB points there; the process must preload the gcc runtimes.
 SAN_LIB = os.path.join(HERE, "libsparsepr_san.so")
 HOST_SAN_FLAGS = ["-O1", "-g", "-fno-omit-frame-pointer", "-fsanitize=address,undefined",
@@ -63,11 +64,13 @@ HOST_SAN_FLAGS = ["-O1", "-g", "-fno-omit-frame-pointer", "-fsanitize=address,un
 
 def build_sanitized() -> str:
     build()
-    api = os.path.join(BUILD, "api_san.o")
+    host = [x for x in SOURCES if x.endswith(".cpp")]
+    apis = [os.path.join(BUILD, os.path.splitext(x)[0] + "_san.o") for x in host]
     host_cc = ["g++", "-std=c++17", "-fPIC", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include"]
-    subprocess.check_call([*host_cc, *HOST_SAN_FLAGS, "-c", os.path.join(CSRC, "api.cpp"), "-o", api])
-    objs = [os.path.join(BUILD, os.path.splitext(s)[0] + ".o") for s in SOURCES if s != "api.cpp"]
-    link = ["g++", "-shared", *HOST_SAN_FLAGS, "-o", SAN_LIB, api, *objs,
+    for src, api in zip(host, apis):
+        subprocess.check_call([*host_cc, *HOST_SAN_FLAGS, "-c", os.path.join(CSRC, src), "-o", api])
+    objs = [os.path.join(BUILD, os.path.splitext(s)[0] + ".o") for s in SOURCES if s not in host]
+    link = ["g++", "-shared", *HOST_SAN_FLAGS, "-o", SAN_LIB, *apis, *objs,
             "-L/opt/rocm/lib", "-lamdhip64", "-Wl,-rpath,/opt/rocm/lib"]
     subprocess.check_call(link)
     return SAN_LIB

@@ -1,0 +1,358 @@
+// Kernels of the operators on a K/V cache for gfx950: attention of new tokens,
+// append, accumulated attention weights, eviction.
+#include <hip/hip_runtime.h>
+#include <float.h>
+#include <limits.h>
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "cache_device.hpp"
+
+namespace sparsepr {
+
+namespace {
+
+constexpr float kNoMax = -FLT_MAX;
+
+// ---- attention --------------------------------------------------------------
+
+// Whether token t sees token u (u < T).
+__device__ __forceinline__ bool token_sees(const CacheCall& c, const int32_t* par, int t, int u) {
+  if (c.mask == SPARSEPR_TOKENS_FULL) return true;
+  if (c.mask == SPARSEPR_TOKENS_CAUSAL) return u <= t;
+  while (t > u) {
+    const int p = par[t];
+    t = p < -1 || p >= t ? -1 : p;
+  }
+  return t == u;
+}
+
+// One block a row: every thread runs an online softmax over each 256th key in
+// registers, the threads' parts are joined at the end.
+template <int D, int BF16>
+__global__ __launch_bounds__(256) void k_cache_attend(CacheCall c) {
+  __shared__ float red[4][D + 2];
+  const int H = c.Hkv * c.G, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int t = blockIdx.x % c.T, bh = blockIdx.x / c.T, b = bh / H, hq = bh % H, hk = hq / c.G;
+  const int n = cache_count(c, b, c.T), len = cache_length(c, b);
+  if (t >= n) return;
+  const int32_t* par = c.parents ? c.parents + (size_t)b * c.T : nullptr;
+  if (par && tid == 0 && (par[t] < -1 || par[t] >= t)) raise_flag(c, b, SPARSEPR_CACHE_FLAG_BAD_INDEX);
+  const int64_t qo = b * c.qsb + hq * c.qsh + t * c.qsn;
+  float m = kNoMax, l = 0.f, O[D];
+#pragma unroll
+  for (int i = 0; i < D; ++i) O[i] = 0.f;
+  const float scale = 1.f / sqrtf((float)D);
+  for (int j = tid; j < len + n; j += 256) {
+    const void *kp = c.k, *vp = c.v;
+    int64_t o = b * c.sb + hk * c.sh + (int64_t)j * c.sn;
+    if (j >= len) {
+      if (!token_sees(c, par, t, j - len)) continue;
+      kp = c.kn;
+      vp = c.vn;
+      o = b * c.nsb + hk * c.nsh + (int64_t)(j - len) * c.nsn;
+    }
+    float s = 0.f;
+    for (int i = 0; i < D; ++i) s = fmaf(load_x(c.q, BF16, qo + i), load_x(kp, BF16, o + i), s);
+    s *= scale;
+    const float mn = fmaxf(m, s), a = expf(m - mn), p = expf(s - mn);
+    m = mn;
+    l = l * a + p;
+#pragma unroll
+    for (int i = 0; i < D; ++i) O[i] = fmaf(p, load_x(vp, BF16, o + i), O[i] * a);
+  }
+  const float mw = wave_max(m), a = expf(m - mw);
+  l = wave_sum(l * a);
+#pragma unroll
+  for (int i = 0; i < D; ++i) {
+    const float o = wave_sum(O[i] * a);
+    if (lane == 0) red[wv][i] = o;
+  }
+  if (lane == 0) red[wv][D] = mw, red[wv][D + 1] = l;
+  __syncthreads();
+  if (tid >= D) return;
+  m = fmaxf(fmaxf(red[0][D], red[1][D]), fmaxf(red[2][D], red[3][D]));
+  float o = 0.f;
+  l = 0.f;
+  for (int w = 0; w < 4; ++w) {
+    const float f = expf(red[w][D] - m);
+    l += red[w][D + 1] * f;
+    o += red[w][tid] * f;
+  }
+  const int64_t oo = b * c.osb + hq * c.osh + t * c.osn + tid;
+  if (BF16)
+    ((uint16_t*)c.out)[oo] = __builtin_bit_cast(uint16_t, (__bf16)(o / l));
+  else
+    ((float*)c.out)[oo] = o / l;
+  if (tid == 0 && c.lse) c.lse[((size_t)b * H + hq) * c.T + t] = m + logf(l);
+}
+
+// ---- append -----------------------------------------------------------------
+
+// Rows to append to entry b, or -1 where they do not fit or the list has a bad
+// index (then `flag` says which).  Called by whole blocks.
+__device__ int rows_to_append(const CacheCall& c, int b, int len, int& flag) {
+  const int n = cache_count(c, b, c.C);
+  int bad = 0;
+  if (c.rows)
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+      const int r = c.rows[(size_t)b * c.C + i];
+      bad |= r < 0 || r >= c.T;
+    }
+  bad = __syncthreads_or(bad);
+  flag = bad ? SPARSEPR_CACHE_FLAG_BAD_INDEX : n > c.cap - len ? SPARSEPR_CACHE_FLAG_OVERFLOW : 0;
+  return flag ? -1 : n;
+}
+
+// Rows of new K and V into the slots behind the used ones, 16 bytes a thread.
+__global__ __launch_bounds__(256) void k_cache_append(CacheCall c, const int32_t* tpos, int32_t* lengths_out) {
+  const int bh = blockIdx.y, b = bh / c.Hkv, hk = bh % c.Hkv;
+  const int es = c.bf16 ? 2 : 4, ch = c.d * es / 16;
+  const int len = cache_length(c, b);
+  int flag;
+  const int n = rows_to_append(c, b, len, flag);
+  if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) {
+    if (flag) raise_flag(c, b, flag);
+    if (lengths_out != c.lengths) lengths_out[b] = len + max(n, 0);
+  }
+  const int i = (blockIdx.x * 256 + threadIdx.x) / ch, part = (blockIdx.x * 256 + threadIdx.x) % ch;
+  if (i >= n) return;
+  const int r = c.rows ? c.rows[(size_t)b * c.C + i] : i;
+  const int64_t src = (b * c.nsb + hk * c.nsh + (int64_t)r * c.nsn) * es + part * 16;
+  const int64_t dst = (b * c.sb + hk * c.sh + (int64_t)(len + i) * c.sn) * es + part * 16;
+  const uint4 kv = *(const uint4*)((const char*)c.kn + src), vv = *(const uint4*)((const char*)c.vn + src);
+  *(uint4*)((char*)const_cast<void*>(c.k) + dst) = kv;
+  *(uint4*)((char*)const_cast<void*>(c.v) + dst) = vv;
+  if (part == 0) {
+    const size_t slot = (size_t)bh * c.cap + len + i;
+    if (c.scores) c.scores[slot] = 0.f;
+    if (c.positions) c.positions[slot] = tpos[(size_t)b * c.T + r];
+  }
+}
+
+// Lengths in place, once every block has read the old ones.
+__global__ __launch_bounds__(256) void k_cache_append_lengths(CacheCall c) {
+  const int b = blockIdx.x, len = cache_length(c, b);
+  int flag;
+  const int n = rows_to_append(c, b, len, flag);
+  if (threadIdx.x == 0) c.lengths[b] = len + max(n, 0);
+}
+
+// ---- accumulate -------------------------------------------------------------
+
+// A thread a slot; the rows one after the other.
+template <int D, int BF16>
+__global__ __launch_bounds__(256) void k_cache_accumulate(CacheCall c) {
+  const int bh = blockIdx.y, b = bh / c.Hkv, hk = bh % c.Hkv;
+  const int n = cache_count(c, b, c.C), len = cache_length(c, b);
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= len) return;
+  const float scale = 1.f / sqrtf((float)D);
+  float kr[D];
+  const int64_t ko = b * c.sb + hk * c.sh + (int64_t)j * c.sn;
+#pragma unroll
+  for (int i = 0; i < D; ++i) kr[i] = load_x(c.k, BF16, ko + i);
+  float sum = 0.f;
+  for (int i = 0; i < n; ++i) {
+    const int r = c.rows ? c.rows[(size_t)b * c.C + i] : i;
+    if (r < 0 || r >= c.T) {
+      if (j == 0) raise_flag(c, b, SPARSEPR_CACHE_FLAG_BAD_INDEX);
+      continue;
+    }
+    if (c.mask != SPARSEPR_TOKENS_FULL && j > (int64_t)len - n + i) continue;
+    for (int g = 0; g < c.G; ++g) {
+      const int hq = hk * c.G + g;
+      const float z = c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + r];
+      if (z == -INFINITY) continue;
+      const int64_t qo = b * c.qsb + hq * c.qsh + (int64_t)r * c.qsn;
+      float s = 0.f;
+#pragma unroll 16
+      for (int x = 0; x < D; ++x) s = fmaf(load_x(c.q, BF16, qo + x), kr[x], s);
+      sum += expf(s * scale - z);
+    }
+  }
+  c.scores[(size_t)bh * c.cap + j] += sum;
+}
+
+// ---- eviction ---------------------------------------------------------------
+
+// Workspace of an eviction: per K/V head the kept slots' sources src[budget],
+// the freed slots hole[budget], and (rows to move, rows kept).
+struct EvictWork {
+  int32_t* src;
+  int32_t* hole;
+  int2* count;
+};
+
+__device__ __forceinline__ uint32_t evict_key(const CacheCall& c, size_t base, int j, int n_sink, int n_recent, int newest) {
+  if (n_sink > 0 || n_recent > 0) {
+    const int p = c.positions[base + j];
+    if (p < n_sink || (n_recent > 0 && (int64_t)p > (int64_t)newest - n_recent)) return 0xffffffffu;
+  }
+  const float f = c.scores[base + j] + 0.f;  // -0 ranks with 0
+  return f != f ? 0xfffffffeu : float_order_bits(f);
+}
+
+// One block a K/V head: the budget-th largest key by four 8-bit digits, then
+// one pass over the slots in order that numbers the freed and the moving ones.
+__global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w, int budget, int n_sink, int n_recent) {
+  __shared__ int hist[256];
+  __shared__ int wsum[3][16], sh_digit, sh_need, sh_newest;
+  const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int len = cache_length(c, bh / c.Hkv);
+  const size_t base = (size_t)bh * c.cap;
+  int32_t* src = w.src + (size_t)bh * budget;
+  int32_t* hole = w.hole + (size_t)bh * budget;
+  if (len <= budget) {
+    for (int j = tid; j < len; j += 1024) src[j] = j;
+    if (tid == 0) w.count[bh] = make_int2(0, len);
+    return;
+  }
+  if (tid == 0) sh_newest = INT_MIN;
+  __syncthreads();
+  if (n_recent > 0) {
+    int m = INT_MIN;
+    for (int j = tid; j < len; j += 1024) m = max(m, c.positions[base + j]);
+    atomicMax(&sh_newest, m);
+    __syncthreads();
+  }
+  const int newest = sh_newest;
+  uint32_t prefix = 0, mask = 0;
+  int need = budget;  // keys still to take among those that match the prefix
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+    for (int j = tid; j < len; j += 1024) {
+      const uint32_t k = evict_key(c, base, j, n_sink, n_recent, newest);
+      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
+    }
+    __syncthreads();
+    if (tid == 0) {
+      int d = 255, left = need;
+      while (hist[d] < left) left -= hist[d--];
+      sh_digit = d;
+      sh_need = left;
+    }
+    __syncthreads();
+    need = sh_need;
+    prefix |= (uint32_t)sh_digit << shift;
+    mask |= 255u << shift;
+    __syncthreads();
+  }
+  // keys above `prefix` stay, and the first `need` that equal it
+  int n_eq = 0, n_hole = 0, n_move = 0;
+  for (int j0 = 0; j0 < len; j0 += 1024) {
+    const int j = j0 + tid;
+    const bool in = j < len;
+    const uint32_t k = in ? evict_key(c, base, j, n_sink, n_recent, newest) : 0;
+    const bool eq = in && k == prefix;
+    const uint64_t before = lane ? ~0ull >> (64 - lane) : 0;
+    const uint64_t beq = __ballot(eq);
+    if (lane == 0) wsum[0][wv] = __popcll(beq);
+    __syncthreads();
+    int req = n_eq + __popcll(beq & before);
+    for (int x = 0; x < 16; ++x) {
+      if (x < wv) req += wsum[0][x];
+      n_eq += wsum[0][x];
+    }
+    const bool keep = in && (k > prefix || (eq && req < need));
+    const bool ho = in && j < budget && !keep, mv = keep && j >= budget;
+    const uint64_t bho = __ballot(ho), bmv = __ballot(mv);
+    if (lane == 0) wsum[1][wv] = __popcll(bho), wsum[2][wv] = __popcll(bmv);
+    __syncthreads();
+    int rho = n_hole + __popcll(bho & before), rmv = n_move + __popcll(bmv & before);
+    for (int x = 0; x < 16; ++x) {
+      if (x < wv) rho += wsum[1][x], rmv += wsum[2][x];
+      n_hole += wsum[1][x];
+      n_move += wsum[2][x];
+    }
+    if (keep && j < budget) src[j] = j;
+    if (ho) hole[rho] = j;
+    __syncthreads();
+    if (mv) src[hole[rmv]] = j;
+  }
+  if (tid == 0) w.count[bh] = make_int2(n_move, budget);
+}
+
+// The kept rows to their slots, 16 bytes of K and of V a thread.
+__global__ __launch_bounds__(256) void k_evict_move(CacheCall c, EvictTo to, EvictWork w, int budget) {
+  const int bh = blockIdx.y, b = bh / c.Hkv, hk = bh % c.Hkv;
+  const int es = c.bf16 ? 2 : 4, ch = c.d * es / 16;
+  const int2 cnt = w.count[bh];
+  const int n = to.in_place ? cnt.x : cnt.y;
+  if (hk == 0 && blockIdx.x == 0 && threadIdx.x == 0) to.lengths[b] = cnt.y;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * ch; i += (int64_t)gridDim.x * 256) {
+    const int r = (int)(i / ch), part = (int)(i % ch);
+    const int dst = to.in_place ? w.hole[(size_t)bh * budget + r] : r;
+    const int src = w.src[(size_t)bh * budget + dst];
+    const int64_t so = (b * c.sb + hk * c.sh + (int64_t)src * c.sn) * es + part * 16;
+    const int64_t po = (b * to.sb + hk * to.sh + (int64_t)dst * to.sn) * es + part * 16;
+    const uint4 kv = *(const uint4*)((const char*)c.k + so), vv = *(const uint4*)((const char*)c.v + so);
+    *(uint4*)((char*)to.k + po) = kv;
+    *(uint4*)((char*)to.v + po) = vv;
+    if (part == 0) {
+      if (to.scores) to.scores[(size_t)bh * to.cap + dst] = c.scores[(size_t)bh * c.cap + src];
+      if (to.positions) to.positions[(size_t)bh * to.cap + dst] = c.positions[(size_t)bh * c.cap + src];
+    }
+  }
+}
+
+EvictWork evict_work(const CacheCall& c, int budget, void* ws) {
+  const size_t n = (size_t)c.B * c.Hkv;
+  char* p = (char*)ws;
+  return {(int32_t*)(p + n * 8), (int32_t*)(p + n * 8) + n * budget, (int2*)p};
+}
+
+template <class F>
+void by_type(const CacheCall& c, F&& f) {
+  if (c.d == 64)
+    c.bf16 ? f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{})
+           : f(std::integral_constant<int, 64>{}, std::integral_constant<int, 0>{});
+  else
+    c.bf16 ? f(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{})
+           : f(std::integral_constant<int, 128>{}, std::integral_constant<int, 0>{});
+}
+
+}  // namespace
+
+size_t cache_attend_workspace(const CacheCall&) { return 0; }
+
+void launch_cache_attend(const CacheCall& c, void*, hipStream_t s) {
+  by_type(c, [&](auto d, auto bf) {
+    k_cache_attend<d.value, bf.value><<<dim3((unsigned)(c.B * c.Hkv * c.G * c.T)), 256, 0, s>>>(c);
+  });
+}
+
+void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int32_t* lengths_out,
+                         hipStream_t s) {
+  const int ch = c.d * (c.bf16 ? 2 : 4) / 16;
+  const unsigned blocks = (unsigned)(((int64_t)c.C * ch + 255) / 256);
+  k_cache_append<<<dim3(blocks, c.B * c.Hkv), 256, 0, s>>>(c, token_positions, lengths_out);
+  if (lengths_out == c.lengths) k_cache_append_lengths<<<c.B, 256, 0, s>>>(c);
+}
+
+size_t cache_accumulate_workspace(const CacheCall&) { return 0; }
+
+void launch_cache_accumulate(const CacheCall& c, void*, hipStream_t s) {
+  by_type(c, [&](auto d, auto bf) {
+    k_cache_accumulate<d.value, bf.value><<<dim3((c.cap + 255) / 256, c.B * c.Hkv), 256, 0, s>>>(c);
+  });
+}
+
+size_t cache_evict_workspace(const CacheCall& c, int budget) {
+  return (size_t)c.B * c.Hkv * (8 + 8 * (size_t)budget);
+}
+
+void launch_cache_evict(const CacheCall& c, const EvictTo& to, int budget, int n_sink,
+                        int n_recent, void* ws, hipStream_t s) {
+  const EvictWork w = evict_work(c, budget, ws);
+  k_evict_select<<<c.B * c.Hkv, 1024, 0, s>>>(c, w, budget, n_sink, n_recent);
+  const int ch = c.d * (c.bf16 ? 2 : 4) / 16;
+  const int64_t most = to.in_place ? std::min(budget, std::max(c.cap - budget, 1)) : budget;
+  const unsigned blocks = (unsigned)std::min<int64_t>((most * ch + 255) / 256, 256);
+  k_evict_move<<<dim3(blocks, c.B * c.Hkv), 256, 0, s>>>(c, to, w, budget);
+}
+
+}  // namespace sparsepr

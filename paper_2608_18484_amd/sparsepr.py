@@ -63,6 +63,27 @@ class Timings(ctypes.Structure):
 
 
 _P = ctypes.c_void_p
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads_kv", ctypes.c_int32),
+                ("capacity", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_n", ctypes.c_int64), ("dtype", ctypes.c_int32), ("k", _P), ("v", _P),
+                ("lengths", _P), ("scores", _P), ("positions", _P), ("flags", _P)]
+
+
+class Tokens(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("n", ctypes.c_int32),
+                ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_n", ctypes.c_int64), ("out_stride_b", ctypes.c_int64),
+                ("out_stride_h", ctypes.c_int64), ("out_stride_n", ctypes.c_int64),
+                ("kv_stride_b", ctypes.c_int64), ("kv_stride_h", ctypes.c_int64),
+                ("kv_stride_n", ctypes.c_int64), ("mask", ctypes.c_int32)]
+
+
+TOKENS_CAUSAL, TOKENS_FULL, TOKENS_TREE = 0, 1, 2
+CACHE_FLAG_OVERFLOW, CACHE_FLAG_BAD_INDEX = 1, 2
 HOST_FIELDS = [
     ("labels_q", "i4"), ("labels_kv", "i4"), ("routes", "u1"), ("probes", "i4"),
     ("n_probes", None),
@@ -83,7 +104,11 @@ EXPORTED = ["sparsepr_params_default", "sparsepr_workspace_size", "sparsepr_plan
             "sparsepr_plan", "sparsepr_attend", "sparsepr_dense_workspace_size",
             "sparsepr_dense_attend", "sparsepr_get_stats", "sparsepr_plan_export",
             "sparsepr_plan_import", "sparsepr_set_profiling", "sparsepr_get_timings",
-            "sparsepr_plan_destroy", "sparsepr_last_error", "sparsepr_plan_create_static"]
+            "sparsepr_plan_destroy", "sparsepr_last_error", "sparsepr_plan_create_static",
+            "sparsepr_cache_attend_workspace_size", "sparsepr_cache_attend",
+            "sparsepr_cache_append", "sparsepr_cache_accumulate_workspace_size",
+            "sparsepr_cache_accumulate", "sparsepr_cache_evict_workspace_size",
+            "sparsepr_cache_evict"]
 
 _lib = None
 
@@ -367,3 +392,251 @@ def dense_attention(q, k, v, out=None, stream=None):
     _check(lib().sparsepr_dense_attend(ctypes.byref(sh), _ptr(q), _ptr(k), _ptr(v), _ptr(out),
                                        None, ctypes.c_size_t(0), _stream(stream)))
     return out
+
+
+def _tensor(name, t, shape, dtype, device, contiguous=True):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if t.device != device:
+        raise ValueError(f"{name}: tensor on {t.device}, the cache is on {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    if not contiguous and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: last dimension must be contiguous")
+
+
+def _opt(t):
+    return None if t is None else t.data_ptr()
+
+
+class KVCache:
+    """A cache of keys and values with the operators on it (the cache section
+    of include/sparsepr.h): attention of new tokens, append, accumulated
+    attention weights, eviction.  The tensors are the caller's:
+
+      k, v       [B, H_kv, capacity, d] bfloat16 or float32, last dim contiguous,
+                 equal strides
+      lengths    [B] int32: slots in use
+      scores     [B, H_kv, capacity] float32 contiguous, or None: accumulated
+                 weights (accumulate, evict)
+      positions  [B, H_kv, capacity] int32 contiguous, or None: token positions
+                 (evict's n_sink and n_recent)
+
+    Calls are enqueued on `stream` (default: the current stream of the cache's
+    device) and never synchronise; flags() does."""
+
+    def __init__(self, k, v, lengths, scores=None, positions=None):
+        import torch
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k: expected a [B, H_kv, capacity, d] torch.Tensor")
+        if k.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"k: dtype {k.dtype}, expected bfloat16 or float32")
+        if k.device.type != self._device_type:
+            raise ValueError(f"k: tensor on {k.device}, expected a {self._device_type} tensor")
+        self.device, self.dtype = k.device, k.dtype
+        b, hkv, cap, d = k.shape
+        _tensor("k", k, k.shape, k.dtype, k.device, contiguous=False)
+        _tensor("v", v, k.shape, k.dtype, k.device, contiguous=False)
+        if any(n > 1 and x != y for n, x, y in zip(k.shape, k.stride(), v.stride())):
+            raise ValueError(f"v: strides {v.stride()}, those of k are {k.stride()}")
+        _tensor("lengths", lengths, (b,), torch.int32, k.device)
+        if scores is not None:
+            _tensor("scores", scores, (b, hkv, cap), torch.float32, k.device)
+        if positions is not None:
+            _tensor("positions", positions, (b, hkv, cap), torch.int32, k.device)
+        self.k, self.v, self.lengths = k, v, lengths
+        self.scores, self.positions = scores, positions
+        self._flags = torch.zeros(b, dtype=torch.int32, device=k.device)
+        sb, sh, sn, _ = k.stride()
+        self.desc = Cache(b, hkv, cap, d, sb, sh, sn, BF16 if k.dtype == torch.bfloat16 else F32,
+                          k.data_ptr(), v.data_ptr(), lengths.data_ptr(), _opt(scores),
+                          _opt(positions), self._flags.data_ptr())
+
+    _device_type = "cuda"
+
+    def flags(self) -> list:
+        """CACHE_FLAG_* raised on the device since the last call, per batch
+        entry; clears them.  Waits for the device."""
+        import torch
+        torch.cuda.synchronize(self.device)
+        got = self._flags.tolist()
+        self._flags.zero_()
+        torch.cuda.synchronize(self.device)
+        return got
+
+    # -- marshalling --------------------------------------------------------
+
+    def _on(self, stream):
+        """The stream, and a context that makes it and its device current where
+        they are not, so that scratch memory belongs to the stream that uses it."""
+        import contextlib
+
+        import torch
+        if stream is None:
+            s = torch.cuda.current_stream(self.device)
+            if self.device.index == torch.cuda.current_device():
+                return s, contextlib.nullcontext()
+            return s, torch.cuda.device(self.device)
+        if stream.device != self.device:
+            raise ValueError(f"stream on {stream.device}, the cache is on {self.device}")
+        return stream, torch.cuda.stream(stream)
+
+    def _scratch(self, size_fn, *args):
+        """Scratch memory of one call from torch's allocator (None if it needs none)."""
+        import torch
+        need = ctypes.c_size_t(0)
+        _check(size_fn(ctypes.byref(self.desc), *args, ctypes.byref(need)))
+        if need.value == 0:
+            return None, 0
+        return torch.empty(need.value, dtype=torch.uint8, device=self.device), need.value
+
+    def _q(self, q):
+        import torch
+        c = self.desc
+        if not isinstance(q, torch.Tensor) or q.dim() != 4:
+            raise ValueError("q: expected a [B, H, n, d] torch.Tensor")
+        h, n = q.shape[1], q.shape[2]
+        _tensor("q", q, (c.batch, h, n, c.d), self.dtype, self.device, contiguous=False)
+        if n < 1 or h < 1 or h % c.heads_kv != 0:
+            raise ValueError(f"q: {h} heads of {n} tokens; heads must be a multiple of the "
+                             f"cache's {c.heads_kv}, tokens at least 1")
+        return h, n
+
+    def _new(self, k_new, v_new, n):
+        c = self.desc
+        _tensor("k_new", k_new, (c.batch, c.heads_kv, n, c.d), self.dtype, self.device, False)
+        _tensor("v_new", v_new, k_new.shape, self.dtype, self.device, False)
+        if any(m > 1 and x != y for m, x, y in zip(k_new.shape, k_new.stride(), v_new.stride())):
+            raise ValueError(f"v_new: strides {v_new.stride()}, those of k_new are {k_new.stride()}")
+        return k_new.stride()[:3]
+
+    def _list(self, rows, counts, n):
+        """Checks an accepted-rows list and the counts; the list's width."""
+        import torch
+        b, width = self.desc.batch, n
+        if rows is not None:
+            if not isinstance(rows, torch.Tensor) or rows.dim() != 2 or rows.shape[1] < 1:
+                raise ValueError("rows: expected a [B, n_rows] torch.Tensor")
+            width = rows.shape[1]
+            _tensor("rows", rows, (b, width), torch.int32, self.device)
+        if counts is not None:
+            _tensor("counts", counts, (b,), torch.int32, self.device)
+        return width
+
+    # -- operators ----------------------------------------------------------
+
+    def attend(self, q, k_new, v_new, parents=None, counts=None, causal=True, out=None, lse=None,
+               stream=None):
+        """Attention of the new tokens q [B, H, n, d] (their keys and values
+        k_new, v_new [B, H_kv, n, d]) over the slots in use and each other; see
+        sparsepr_cache_attend.  parents [B, n] int32 makes them a tree; without
+        it they are a chain (causal) or all see each other.  counts [B] int32:
+        tokens of each entry.  Returns (out, lse); rows behind counts keep what
+        the given out and lse hold (zeros where they are made here)."""
+        import torch
+        h, n = self._q(q)
+        ks = self._new(k_new, v_new, n)
+        b = self.desc.batch
+        self._list(None, counts, n)
+        mask = TOKENS_CAUSAL if causal else TOKENS_FULL
+        if parents is not None:
+            if not causal:
+                raise ValueError("parents: a tree's tokens see their ancestors only (causal=True)")
+            _tensor("parents", parents, (b, n), torch.int32, self.device)
+            mask = TOKENS_TREE
+        if out is not None:
+            _tensor("out", out, q.shape, self.dtype, self.device, contiguous=False)
+        if lse is not None:
+            _tensor("lse", lse, (b, h, n), torch.float32, self.device)
+        s, ctx = self._on(stream)
+        with ctx:
+            make = torch.empty if counts is None else torch.zeros
+            if out is None:
+                out = make(q.shape, dtype=self.dtype, device=self.device)
+            if lse is None:
+                lse = make((b, h, n), dtype=torch.float32, device=self.device)
+            t = Tokens(h, n, *q.stride()[:3], *out.stride()[:3], *ks, mask)
+            L = lib()
+            ws, nbytes = self._scratch(L.sparsepr_cache_attend_workspace_size, ctypes.byref(t))
+            _check(L.sparsepr_cache_attend(
+                ctypes.byref(self.desc), ctypes.byref(t), _ptr(q), _ptr(k_new), _ptr(v_new),
+                _P(_opt(parents)), _P(_opt(counts)), _ptr(out), _ptr(lse), _P(_opt(ws)),
+                ctypes.c_size_t(nbytes), _P(s.cuda_stream)))
+        return out, lse
+
+    def append(self, k_new, v_new, positions=None, rows=None, counts=None, lengths_out=None,
+               stream=None):
+        """Append the rows of k_new, v_new [B, H_kv, n, d] named by rows [B, n_rows]
+        int32 (None: all, in order), counts[b] of them, behind the slots in use;
+        see sparsepr_cache_append.  positions [B, n] int32: the tokens'
+        positions (with a cache that keeps them).  The new lengths go to
+        lengths_out [B] int32, or into the cache's own."""
+        import torch
+        if not isinstance(k_new, torch.Tensor) or k_new.dim() != 4 or k_new.shape[2] < 1:
+            raise ValueError("k_new: expected a [B, H_kv, n, d] torch.Tensor with n >= 1")
+        c, n = self.desc, k_new.shape[2]
+        ks = self._new(k_new, v_new, n)
+        width = self._list(rows, counts, n)
+        if (positions is None) != (self.positions is None):
+            raise ValueError("positions: given when the cache has positions, and only then")
+        if positions is not None:
+            _tensor("positions", positions, (c.batch, n), torch.int32, self.device)
+        if lengths_out is None:
+            lengths_out = self.lengths
+        _tensor("lengths_out", lengths_out, (c.batch,), torch.int32, self.device)
+        s, ctx = self._on(stream)
+        with ctx:
+            t = Tokens(c.heads_kv, n, 0, 0, 0, 0, 0, 0, *ks, TOKENS_CAUSAL)
+            _check(lib().sparsepr_cache_append(
+                ctypes.byref(c), ctypes.byref(t), _ptr(k_new), _ptr(v_new), _P(_opt(positions)),
+                _P(_opt(rows)), ctypes.c_int32(width), _P(_opt(counts)), _ptr(lengths_out),
+                _P(s.cuda_stream)))
+
+    def accumulate(self, q, lse, rows=None, counts=None, causal=True, stream=None):
+        """Add the attention weights of the rows that were just appended (rows
+        and counts as in append; q and lse as in attend) to the scores of the
+        slots that they see; see sparsepr_cache_accumulate."""
+        import torch
+        h, n = self._q(q)
+        c = self.desc
+        width = self._list(rows, counts, n)
+        _tensor("lse", lse, (c.batch, h, n), torch.float32, self.device)
+        if self.scores is None:
+            raise ValueError("accumulate: the cache has no scores")
+        s, ctx = self._on(stream)
+        with ctx:
+            t = Tokens(h, n, *q.stride()[:3], 0, 0, 0, 0, 0, 0,
+                       TOKENS_CAUSAL if causal else TOKENS_FULL)
+            L = lib()
+            ws, nbytes = self._scratch(L.sparsepr_cache_accumulate_workspace_size,
+                                       ctypes.byref(t), ctypes.c_int32(width))
+            _check(L.sparsepr_cache_accumulate(
+                ctypes.byref(c), ctypes.byref(t), _ptr(q), _ptr(lse), _P(_opt(rows)),
+                ctypes.c_int32(width), _P(_opt(counts)), _P(_opt(ws)), ctypes.c_size_t(nbytes),
+                _P(s.cuda_stream)))
+
+    def evict(self, budget, n_sink=0, n_recent=0, out=None, stream=None):
+        """Keep at most `budget` slots of every K/V head: the first n_sink
+        positions, the n_recent newest and the largest scores, in place or in
+        another KVCache `out`; see sparsepr_cache_evict."""
+        if self.scores is None:
+            raise ValueError("evict: the cache has no scores")
+        if out is not None and out.device != self.device:
+            raise ValueError(f"out: cache on {out.device}, this one on {self.device}")
+        for name, x in (("budget", budget), ("n_sink", n_sink), ("n_recent", n_recent)):
+            if not 0 <= x < 2 ** 31:
+                raise ValueError(f"{name}: {x} is out of range")
+        s, ctx = self._on(stream)
+        with ctx:
+            L = lib()
+            ws, nbytes = self._scratch(L.sparsepr_cache_evict_workspace_size,
+                                       ctypes.c_int32(budget))
+            _check(L.sparsepr_cache_evict(
+                ctypes.byref(self.desc), None if out is None else ctypes.byref(out.desc),
+                ctypes.c_int32(budget), ctypes.c_int32(n_sink), ctypes.c_int32(n_recent),
+                _P(_opt(ws)), ctypes.c_size_t(nbytes), _P(s.cuda_stream)))

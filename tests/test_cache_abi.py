@@ -1,0 +1,294 @@
+"""Host-side checks of the operators on a K/V cache: struct layout, and what
+their entry points refuse before any HIP call."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from paper_2608_18484_amd import sparsepr as S
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "sparsepr.h")
+P = 1 << 20  # stands for an aligned device pointer; nothing reads through it
+
+
+def test_struct_layout_matches_c_compiler(tmp_path):
+    structs = {"sparsepr_cache": S.Cache, "sparsepr_tokens": S.Tokens}
+    lines = ['#include <stdio.h>', '#include <stddef.h>', f'#include "{HEADER}"', 'int main(void) {']
+    for cname, cls in structs.items():
+        lines.append(f'printf("{cname} %zu\\n", sizeof({cname}));')
+        for fname, _ in cls._fields_:
+            lines.append(f'printf("{cname}.{fname} %zu\\n", offsetof({cname}, {fname}));')
+    lines.append("return 0; }")
+    src = tmp_path / "layout.c"
+    src.write_text("\n".join(lines))
+    exe = tmp_path / "layout"
+    subprocess.check_call(["gcc", "-o", str(exe), str(src)])
+    got = dict(l.split() for l in subprocess.check_output([str(exe)], text=True).splitlines())
+    for cname, cls in structs.items():
+        assert int(got[cname]) == ctypes.sizeof(cls), cname
+        for fname, _ in cls._fields_:
+            assert int(got[f"{cname}.{fname}"]) == getattr(cls, fname).offset, (cname, fname)
+
+
+def cache(**kw):
+    base = dict(batch=2, heads_kv=4, capacity=100, d=64, stride_b=4 * 100 * 64, stride_h=100 * 64,
+                stride_n=64, dtype=S.BF16, k=P, v=2 * P, lengths=3 * P, scores=4 * P,
+                positions=5 * P, flags=None)
+    base.update(kw)
+    return S.Cache(**base)
+
+
+def tokens(**kw):
+    base = dict(heads=8, n=5, stride_b=8 * 5 * 64, stride_h=5 * 64, stride_n=64,
+                out_stride_b=8 * 5 * 64, out_stride_h=5 * 64, out_stride_n=64,
+                kv_stride_b=4 * 5 * 64, kv_stride_h=5 * 64, kv_stride_n=64, mask=S.TOKENS_CAUSAL)
+    base.update(kw)
+    return S.Tokens(**base)
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def attend_size(c, t):
+    n = ctypes.c_size_t(0)
+    st = S.lib().sparsepr_cache_attend_workspace_size(_ref(c), _ref(t), ctypes.byref(n))
+    return st, n.value, S.lib().sparsepr_last_error().decode()
+
+
+def vp(x):
+    return ctypes.c_void_p(x)
+
+
+def attend(c, t, q=P, kn=P, vn=P, parents=None, counts=None, out=7 * P, lse=None, ws=P,
+           nbytes=1 << 40):
+    st = S.lib().sparsepr_cache_attend(_ref(c), _ref(t), vp(q), vp(kn), vp(vn), vp(parents),
+                                       vp(counts), vp(out), vp(lse), vp(ws),
+                                       ctypes.c_size_t(nbytes), None)
+    return st, S.lib().sparsepr_last_error().decode()
+
+
+def append(c, t, kn=P, vn=P, pos=P, rows=None, n_rows=5, counts=None, lengths_out=3 * P):
+    st = S.lib().sparsepr_cache_append(_ref(c), _ref(t), vp(kn), vp(vn), vp(pos), vp(rows),
+                                       ctypes.c_int32(n_rows), vp(counts), vp(lengths_out), None)
+    return st, S.lib().sparsepr_last_error().decode()
+
+
+def accumulate(c, t, q=P, lse=P, rows=None, n_rows=5, counts=None, ws=P, nbytes=1 << 40):
+    st = S.lib().sparsepr_cache_accumulate(_ref(c), _ref(t), vp(q), vp(lse), vp(rows),
+                                           ctypes.c_int32(n_rows), vp(counts), vp(ws),
+                                           ctypes.c_size_t(nbytes), None)
+    return st, S.lib().sparsepr_last_error().decode()
+
+
+def evict(c, to=None, budget=50, n_sink=0, n_recent=0, ws=P, nbytes=1 << 40):
+    st = S.lib().sparsepr_cache_evict(_ref(c), _ref(to), ctypes.c_int32(budget),
+                                      ctypes.c_int32(n_sink), ctypes.c_int32(n_recent), vp(ws),
+                                      ctypes.c_size_t(nbytes), None)
+    return st, S.lib().sparsepr_last_error().decode()
+
+
+def test_attend_workspace_depends_on_geometry_alone():
+    st, n, _ = attend_size(cache(k=None, v=None, lengths=None), tokens())
+    assert st == 0
+    assert attend_size(cache(), tokens())[:2] == (0, n)
+
+
+@pytest.mark.parametrize("ckw,tkw,status,needle", [
+    (dict(batch=0), {}, 1, "batch"),
+    (dict(heads_kv=0), {}, 1, "heads_kv"),
+    (dict(capacity=0), {}, 1, "capacity"),
+    (dict(dtype=2), {}, 1, "dtype"),
+    (dict(d=96), {}, 2, "64 or 128"),
+    (dict(capacity=(1 << 28) + 1), {}, 2, "2^28"),
+    (dict(batch=20000), {}, 2, "65535"),
+    (dict(stride_n=32), {}, 1, "overlap"),
+    (dict(stride_h=99 * 64), {}, 1, "overlap"),
+    (dict(stride_b=0), {}, 1, "overlap"),
+    (dict(stride_n=68, stride_h=68 * 100, stride_b=68 * 400), {}, 2, "16 bytes"),
+    ({}, dict(n=0), 1, "n must"),
+    ({}, dict(heads=6), 1, "multiple"),
+    ({}, dict(heads=0), 1, "multiple"),
+    ({}, dict(mask=3), 1, "mask"),
+    ({}, dict(n=257, mask=2), 2, "256"),
+    ({}, dict(n=1 << 28), 2, "2^28"),
+    ({}, dict(stride_n=-64), 1, "Q strides"),
+    ({}, dict(stride_n=65), 2, "Q strides"),
+    ({}, dict(kv_stride_n=-64), 1, "K/V strides"),
+    ({}, dict(kv_stride_h=4), 2, "K/V strides"),
+    ({}, dict(out_stride_n=0), 1, "output strides"),
+    ({}, dict(out_stride_n=66, out_stride_h=66 * 5, out_stride_b=66 * 40), 2, "output strides"),
+])
+def test_attend_geometry_refused(ckw, tkw, status, needle):
+    st, _, msg = attend_size(cache(**ckw), tokens(**tkw))
+    assert st == status and needle in msg
+    st, msg = attend(cache(**ckw), tokens(**tkw))
+    assert st == status and needle in msg
+
+
+def test_strides_of_extent_one_are_free():
+    one = cache(batch=1, heads_kv=1, stride_b=3, stride_h=5)
+    assert attend_size(one, tokens(heads=1, n=1, stride_b=1, stride_h=1, stride_n=1,
+                                   out_stride_b=0, out_stride_h=0, out_stride_n=0,
+                                   kv_stride_b=1, kv_stride_h=1, kv_stride_n=1))[0] == 0
+
+
+def test_null_and_misaligned_pointers_refused():
+    c, t = cache(), tokens()
+    assert attend(None, t)[0] == 1 and attend(c, None)[0] == 1
+    assert S.lib().sparsepr_cache_attend_workspace_size(_ref(c), _ref(t), None) == 1
+    assert S.lib().sparsepr_cache_accumulate_workspace_size(_ref(c), _ref(t), 5, None) == 1
+    assert S.lib().sparsepr_cache_evict_workspace_size(_ref(c), 5, None) == 1
+    for kw in (dict(q=None), dict(kn=None), dict(vn=None), dict(out=None)):
+        st, msg = attend(c, t, **kw)
+        assert st == 1 and "NULL" in msg
+    for kw in (dict(q=P + 8), dict(kn=P + 2), dict(vn=P + 4), dict(out=P + 8)):
+        st, msg = attend(c, t, **kw)
+        assert st == 2 and "16-byte" in msg
+    for kw in (dict(k=None), dict(v=None), dict(lengths=None)):
+        for f in (lambda x: attend(x, t), lambda x: append(x, t), lambda x: accumulate(x, t), evict):
+            st, msg = f(cache(**kw))
+            assert st == 1 and "NULL" in msg
+    assert attend(cache(k=P + 8), t)[0] == 2
+    # a tree needs parents, the other masks none
+    assert attend(c, tokens(mask=2))[0] == 1
+    assert attend(c, t, parents=P)[0] == 1
+    for kw in (dict(kn=None), dict(vn=None), dict(lengths_out=None), dict(pos=None)):
+        assert append(c, t, **kw)[0] == 1
+    assert append(cache(positions=None), t)[0] == 1
+    assert append(c, t, kn=P + 4)[0] == 2
+    for kw in (dict(q=None), dict(lse=None)):
+        assert accumulate(c, t, **kw)[0] == 1
+    assert accumulate(c, t, q=P + 4)[0] == 2
+
+
+def test_lists_and_scores_refused():
+    c, t = cache(), tokens()
+    for f in (append, accumulate):
+        st, msg = f(c, t, n_rows=0)
+        assert st == 1 and "n_rows" in msg
+        st, msg = f(c, t, n_rows=4)  # all tokens are 5
+        assert st == 1 and "n_rows" in msg
+        st, msg = f(c, t, rows=P, n_rows=1 << 28) if f is accumulate else (2, "2^28")
+        assert st == 2 and "2^28" in msg
+    st, msg = accumulate(cache(scores=None), t)
+    assert st == 1 and "scores" in msg
+    st, msg = evict(cache(scores=None))
+    assert st == 1 and "scores" in msg
+
+
+@pytest.mark.parametrize("kw,needle", [
+    (dict(budget=0), "budget"), (dict(budget=101), "budget"), (dict(n_sink=-1), "n_sink"),
+    (dict(n_recent=-1), "n_recent"), (dict(n_sink=26, n_recent=25), "n_sink"),
+    (dict(n_sink=2 ** 31 - 1, n_recent=2 ** 31 - 1), "n_sink"),
+])
+def test_evict_ranges_refused(kw, needle):
+    st, msg = evict(cache(), **kw)
+    assert st == 1 and needle in msg
+
+
+def test_evict_targets_refused():
+    c = cache()
+    other = dict(k=11 * P, v=12 * P, lengths=13 * P, scores=14 * P, positions=15 * P)
+    assert evict(cache(positions=None), n_recent=1)[0] == 1
+    for kw in (dict(batch=1), dict(heads_kv=2, stride_b=200 * 64), dict(dtype=S.F32),
+               dict(d=128, stride_n=128, stride_h=12800, stride_b=51200)):
+        st, msg = evict(c, cache(**{**other, **kw}))
+        assert st == 1 and "same batch" in msg
+    for name in other:
+        st, msg = evict(c, cache(**{**other, name: getattr(c, name)}))
+        assert st == 1 and "share" in msg
+    st, msg = evict(c, cache(capacity=40, **other))
+    assert st == 1 and "budget" in msg
+
+
+def test_workspaces_checked():
+    c, t = cache(), tokens()
+    n = ctypes.c_size_t(0)
+    assert S.lib().sparsepr_cache_evict_workspace_size(_ref(c), 50, ctypes.byref(n)) == 0
+    assert n.value > 0
+    st, msg = evict(c, nbytes=n.value - 1)
+    assert st == 3 and "needs" in msg
+    assert evict(c, ws=None)[0] == 1
+    assert evict(c, ws=P + 8)[0] == 1
+    st, need, _ = attend_size(c, t)
+    if need:
+        assert attend(c, t, nbytes=need - 1)[0] == 3
+        assert attend(c, t, ws=None)[0] == 1
+
+
+# --- the binding ------------------------------------------------------------
+
+torch = pytest.importorskip("torch")
+
+
+class HostCache(S.KVCache):
+    """The binding's checks on host tensors (they come before any launch)."""
+    _device_type = "cpu"
+
+
+def host_cache(**kw):
+    t = dict(k=torch.zeros(2, 4, 100, 64), v=torch.zeros(2, 4, 100, 64),
+             lengths=torch.zeros(2, dtype=torch.int32), scores=torch.zeros(2, 4, 100),
+             positions=torch.zeros(2, 4, 100, dtype=torch.int32))
+    t.update(kw)
+    return HostCache(**t)
+
+
+@pytest.mark.parametrize("kw,needle", [
+    (dict(k=torch.zeros(2, 4, 100)), "k:"),
+    (dict(k=torch.zeros(2, 4, 100, 64, dtype=torch.float16)), "dtype"),
+    (dict(v=torch.zeros(2, 4, 99, 64)), "v: shape"),
+    (dict(v=torch.zeros(2, 4, 100, 64, dtype=torch.bfloat16)), "v: dtype"),
+    (dict(v=torch.zeros(2, 100, 4, 64).transpose(1, 2)), "strides"),
+    (dict(lengths=torch.zeros(2, dtype=torch.int64)), "lengths: dtype"),
+    (dict(lengths=torch.zeros(3, dtype=torch.int32)), "lengths: shape"),
+    (dict(scores=torch.zeros(2, 4, 100, dtype=torch.float64)), "scores: dtype"),
+    (dict(scores=torch.zeros(2, 4, 200)[:, :, ::2]), "scores: must be contiguous"),
+    (dict(positions=torch.zeros(2, 4, 100)), "positions: dtype"),
+    (dict(k=torch.zeros(2, 4, 64, 100).transpose(2, 3)), "last dimension"),
+])
+def test_binding_refuses_cache_tensors(kw, needle):
+    with pytest.raises(ValueError, match=needle):
+        host_cache(**kw)
+
+
+def test_binding_refuses_host_cache():
+    with pytest.raises(ValueError, match="expected a cuda tensor"):
+        S.KVCache(torch.zeros(2, 4, 100, 64), torch.zeros(2, 4, 100, 64),
+                  torch.zeros(2, dtype=torch.int32))
+
+
+def test_binding_refuses_call_tensors():
+    c = host_cache()
+    q, kn = torch.zeros(2, 8, 5, 64), torch.zeros(2, 4, 5, 64)
+    i32 = dict(dtype=torch.int32)
+    bad = [
+        (lambda: c.attend(q[:, :6], kn, kn), "multiple"),
+        (lambda: c.attend(q[:, :, :0], kn[:, :, :0], kn[:, :, :0]), "at least 1"),
+        (lambda: c.attend(q.bfloat16(), kn, kn), "q: dtype"),
+        (lambda: c.attend(q[:1], kn, kn), "q: shape"),
+        (lambda: c.attend(q, kn[:, :2], kn), "k_new: shape"),
+        (lambda: c.attend(q, kn, kn[:, :, :4]), "v_new: shape"),
+        (lambda: c.attend(q, kn, torch.zeros(2, 5, 4, 64).transpose(1, 2)), "v_new: strides"),
+        (lambda: c.attend(q, kn, kn, parents=torch.zeros(2, 5)), "parents: dtype"),
+        (lambda: c.attend(q, kn, kn, parents=torch.zeros(2, 5, **i32), causal=False), "parents"),
+        (lambda: c.attend(q, kn, kn, counts=torch.zeros(3, **i32)), "counts: shape"),
+        (lambda: c.attend(q, kn, kn, out=torch.zeros(2, 8, 4, 64)), "out: shape"),
+        (lambda: c.attend(q, kn, kn, lse=torch.zeros(2, 8, 10)[:, :, ::2]), "lse: must be"),
+        (lambda: c.append(kn, kn), "positions"),
+        (lambda: c.append(kn, kn, positions=torch.zeros(2, 4, **i32)), "positions: shape"),
+        (lambda: c.append(kn, kn, positions=torch.zeros(2, 5, **i32), rows=torch.zeros(2, 0, **i32)),
+         "rows"),
+        (lambda: c.append(kn, kn, positions=torch.zeros(2, 5, **i32),
+                          lengths_out=torch.zeros(2)), "lengths_out: dtype"),
+        (lambda: c.accumulate(q, torch.zeros(2, 8, 4)), "lse: shape"),
+        (lambda: host_cache(scores=None).accumulate(q, torch.zeros(2, 8, 5)), "scores"),
+        (lambda: host_cache(scores=None).evict(5), "scores"),
+        (lambda: c.evict(1 << 33), "budget"),
+    ]
+    for f, needle in bad:
+        with pytest.raises(ValueError, match=needle):
+            f()

@@ -16,6 +16,8 @@ using namespace sparsepr;
 namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 28;
+// The kernels address the 32 rows of a key tile by 32-bit byte offsets.
+constexpr int64_t kMaxRowStride = int64_t(1) << 24;
 
 sparsepr_status bad(const char* msg) { return set_error(SPARSEPR_ERR_INVALID_ARGUMENT, msg); }
 sparsepr_status unsupported(const char* msg) { return set_error(SPARSEPR_ERR_UNSUPPORTED, msg); }
@@ -75,6 +77,7 @@ sparsepr_status cache_ok(const sparsepr_cache* c, CacheCall& x) {
   if (c->d != 64 && c->d != 128) return unsupported("cache: d must be 64 or 128");
   if (c->capacity > kMaxRows) return unsupported("cache: capacity above 2^28");
   if ((int64_t)c->batch * c->heads_kv > 65535) return unsupported("cache: batch * heads_kv above 65535");
+  if (c->capacity > 1 && c->stride_n > kMaxRowStride) return unsupported("cache: stride_n above 2^24");
   const int es = c->dtype == SPARSEPR_BF16 ? 2 : 4;
   if (!disjoint(c->d, c->batch, c->stride_b, c->heads_kv, c->stride_h, c->capacity, c->stride_n))
     return bad("cache: strides make rows overlap");
@@ -139,6 +142,7 @@ sparsepr_status q_ok(const CacheCall& x) {
 
 sparsepr_status new_kv_ok(const CacheCall& x) {
   if (!in_reach(x.B, x.nsb, x.Hkv, x.nsh, x.T, x.nsn)) return bad("tokens: K/V strides out of range");
+  if (x.T > 1 && x.nsn > kMaxRowStride) return unsupported("tokens: kv_stride_n above 2^24");
   if (!strides16(elem(x), x.B, x.nsb, x.Hkv, x.nsh, x.T, x.nsn))
     return unsupported("tokens: K/V strides must be multiples of 16 bytes");
   return SPARSEPR_OK;

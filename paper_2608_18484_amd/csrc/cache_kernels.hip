@@ -31,8 +31,9 @@ __device__ __forceinline__ bool token_sees(const CacheCall& c, const int32_t* pa
 
 // One block a row: every thread runs an online softmax over each 256th key in
 // registers, the threads' parts are joined at the end.
-template <int D, int BF16>
-__global__ __launch_bounds__(256) void k_cache_attend(CacheCall c) {
+template <int D>
+__global__ __launch_bounds__(256) void k_cache_attend_f32(CacheCall c) {
+  constexpr int BF16 = 0;
   __shared__ float red[4][D + 2];
   const int H = c.Hkv * c.G, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int t = blockIdx.x % c.T, bh = blockIdx.x / c.T, b = bh / H, hq = bh % H, hk = hq / c.G;
@@ -81,11 +82,7 @@ __global__ __launch_bounds__(256) void k_cache_attend(CacheCall c) {
     l += red[w][D + 1] * f;
     o += red[w][tid] * f;
   }
-  const int64_t oo = b * c.osb + hq * c.osh + t * c.osn + tid;
-  if (BF16)
-    ((uint16_t*)c.out)[oo] = __builtin_bit_cast(uint16_t, (__bf16)(o / l));
-  else
-    ((float*)c.out)[oo] = o / l;
+  ((float*)c.out)[b * c.osb + hq * c.osh + t * c.osn + tid] = o / l;
   if (tid == 0 && c.lse) c.lse[((size_t)b * H + hq) * c.T + t] = m + logf(l);
 }
 
@@ -317,12 +314,16 @@ void by_type(const CacheCall& c, F&& f) {
 
 }  // namespace
 
-size_t cache_attend_workspace(const CacheCall&) { return 0; }
+size_t cache_attend_workspace(const CacheCall& c) { return c.bf16 ? cache_attend_workspace_bf16(c) : 0; }
 
-void launch_cache_attend(const CacheCall& c, void*, hipStream_t s) {
-  by_type(c, [&](auto d, auto bf) {
-    k_cache_attend<d.value, bf.value><<<dim3((unsigned)(c.B * c.Hkv * c.G * c.T)), 256, 0, s>>>(c);
-  });
+void launch_cache_attend(const CacheCall& c, void* ws, hipStream_t s) {
+  const unsigned rows = (unsigned)(c.B * c.Hkv * c.G * c.T);
+  if (c.bf16)
+    launch_cache_attend_bf16(c, ws, s);
+  else if (c.d == 64)
+    k_cache_attend_f32<64><<<rows, 256, 0, s>>>(c);
+  else
+    k_cache_attend_f32<128><<<rows, 256, 0, s>>>(c);
 }
 
 void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int32_t* lengths_out,

@@ -108,6 +108,8 @@ def test_attend_workspace_depends_on_geometry_alone():
     (dict(stride_h=99 * 64), {}, 1, "overlap"),
     (dict(stride_b=0), {}, 1, "overlap"),
     (dict(stride_n=68, stride_h=68 * 100, stride_b=68 * 400), {}, 2, "16 bytes"),
+    (dict(stride_n=(1 << 24) + 64, stride_h=1 << 33, stride_b=1 << 36), {}, 2, "2^24"),
+    ({}, dict(kv_stride_n=(1 << 24) + 64), 2, "2^24"),
     ({}, dict(n=0), 1, "n must"),
     ({}, dict(heads=6), 1, "multiple"),
     ({}, dict(heads=0), 1, "multiple"),

@@ -1,5 +1,6 @@
 // Kernels of the operators on a K/V cache for gfx950: attention of new tokens,
-// append, accumulated attention weights, eviction.
+// append, eviction (cache_attn.hip and cache_weigh.hip have the products on the
+// matrix cores).
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <limits.h>
@@ -137,42 +138,6 @@ __global__ __launch_bounds__(256) void k_cache_append_lengths(CacheCall c) {
   if (threadIdx.x == 0) c.lengths[b] = len + max(n, 0);
 }
 
-// ---- accumulate -------------------------------------------------------------
-
-// A thread a slot; the rows one after the other.
-template <int D, int BF16>
-__global__ __launch_bounds__(256) void k_cache_accumulate(CacheCall c) {
-  const int bh = blockIdx.y, b = bh / c.Hkv, hk = bh % c.Hkv;
-  const int n = cache_count(c, b, c.C), len = cache_length(c, b);
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= len) return;
-  const float scale = 1.f / sqrtf((float)D);
-  float kr[D];
-  const int64_t ko = b * c.sb + hk * c.sh + (int64_t)j * c.sn;
-#pragma unroll
-  for (int i = 0; i < D; ++i) kr[i] = load_x(c.k, BF16, ko + i);
-  float sum = 0.f;
-  for (int i = 0; i < n; ++i) {
-    const int r = c.rows ? c.rows[(size_t)b * c.C + i] : i;
-    if (r < 0 || r >= c.T) {
-      if (j == 0) raise_flag(c, b, SPARSEPR_CACHE_FLAG_BAD_INDEX);
-      continue;
-    }
-    if (c.mask != SPARSEPR_TOKENS_FULL && j > (int64_t)len - n + i) continue;
-    for (int g = 0; g < c.G; ++g) {
-      const int hq = hk * c.G + g;
-      const float z = c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + r];
-      if (z == -INFINITY) continue;
-      const int64_t qo = b * c.qsb + hq * c.qsh + (int64_t)r * c.qsn;
-      float s = 0.f;
-#pragma unroll 16
-      for (int x = 0; x < D; ++x) s = fmaf(load_x(c.q, BF16, qo + x), kr[x], s);
-      sum += expf(s * scale - z);
-    }
-  }
-  c.scores[(size_t)bh * c.cap + j] += sum;
-}
-
 // ---- eviction ---------------------------------------------------------------
 
 // Workspace of an eviction: per K/V head the kept slots' sources src[budget],
@@ -302,16 +267,6 @@ EvictWork evict_work(const CacheCall& c, int budget, void* ws) {
   return {(int32_t*)(p + n * 8), (int32_t*)(p + n * 8) + n * budget, (int2*)p};
 }
 
-template <class F>
-void by_type(const CacheCall& c, F&& f) {
-  if (c.d == 64)
-    c.bf16 ? f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{})
-           : f(std::integral_constant<int, 64>{}, std::integral_constant<int, 0>{});
-  else
-    c.bf16 ? f(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{})
-           : f(std::integral_constant<int, 128>{}, std::integral_constant<int, 0>{});
-}
-
 }  // namespace
 
 size_t cache_attend_workspace(const CacheCall& c) { return c.bf16 ? cache_attend_workspace_bf16(c) : 0; }
@@ -332,14 +287,6 @@ void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int
   const unsigned blocks = (unsigned)(((int64_t)c.C * ch + 255) / 256);
   k_cache_append<<<dim3(blocks, c.B * c.Hkv), 256, 0, s>>>(c, token_positions, lengths_out);
   if (lengths_out == c.lengths) k_cache_append_lengths<<<c.B, 256, 0, s>>>(c);
-}
-
-size_t cache_accumulate_workspace(const CacheCall&) { return 0; }
-
-void launch_cache_accumulate(const CacheCall& c, void*, hipStream_t s) {
-  by_type(c, [&](auto d, auto bf) {
-    k_cache_accumulate<d.value, bf.value><<<dim3((c.cap + 255) / 256, c.B * c.Hkv), 256, 0, s>>>(c);
-  });
 }
 
 size_t cache_evict_workspace(const CacheCall& c, int budget) {

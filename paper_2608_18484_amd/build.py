@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsparsepr.so")
 SOURCES = ["plan_kernels.hip", "attn_kernels.hip", "fit_kernels.hip", "cache_attn.hip",
-           "cache_weigh.hip", "cache_kernels.hip", "noalloc.hip", "api.cpp", "cache_api.cpp"]
+           "cache_weigh.hip", "cache_slots.hip", "noalloc.hip", "api.cpp", "cache_api.cpp"]
 ARCH = os.environ.get("SPARSEPR_OFFLOAD_ARCH", "gfx950")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,4 +1,4 @@
-// Attention of new tokens over a K/V cache for gfx950 (bf16).
+// Attention of new tokens over a K/V cache for gfx950.
 //
 // Rows.  The G query heads of a K/V head and the T new tokens are rows
 // r = t * G + g of one product against the same keys; a block owns a tile of
@@ -14,7 +14,7 @@
 // on the device, so a launch fits every length (and a captured graph replays
 // as the cache grows).
 //
-// The tile products are those of dense attention: S^T = K Q^T and
+// The bf16 tile products are those of dense attention: S^T = K Q^T and
 // O^T += V^T P^T on v_mfma_f32_32x32x16_bf16, so that a lane's scores belong
 // to one row; V^T comes from transposing LDS reads.
 #include <hip/hip_runtime.h>
@@ -146,6 +146,57 @@ __device__ __forceinline__ uint32_t odd_bf16(uint32_t x) {  // either half infin
   return (uint32_t)((x & 0x7f80u) == 0x7f80u) | (uint32_t)((x & 0x7f800000u) == 0x7f800000u);
 }
 
+// What a block works on.
+struct Where {
+  int slot, hk, b, parts;     // part, K/V head, entry, the entry's parts
+  int ntok, len, rows, row0;  // the entry's tokens, slots and rows; the tile's first row
+  int tok_end, old_tiles;     // tokens that its rows see at most; tiles of the slots
+  int t_first, t_last;        // key tiles
+};
+
+// Block order: XCD x (block index mod 8) takes the x-th eighth of the parts in
+// use, the row tiles of a part and head next to each other, which read the
+// same keys.
+__device__ __forceinline__ bool locate(const CacheCall& c, const Cut& cut, int tile_rows, int lane, Where& w) {
+  const int per = part_steps(c, cut, lane);
+  const int64_t used = (int64_t)count_parts(c, cut, per, lane) * c.Hkv * cut.row_tiles;
+  const int64_t eighth = (used + 7) / 8;
+  const int64_t at = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
+  if ((int64_t)(blockIdx.x >> 3) >= eighth || at >= used) return false;
+  const int rt = (int)(at % cut.row_tiles), unit = (int)(at / cut.row_tiles);
+  w.hk = unit % c.Hkv;
+  w.slot = unit / c.Hkv;
+  const Part part = find_part(c, cut, per, w.slot, lane);
+  if (part.b < 0 || w.slot >= cut.slots) return false;  // (only if lengths change during the launch)
+  w.b = part.b;
+  w.parts = part.count;
+  w.ntok = cache_count(c, w.b, c.T);
+  w.len = cache_length(c, w.b);
+  w.rows = w.ntok * c.G;
+  w.row0 = rt * tile_rows;
+  if (w.row0 >= w.rows) return false;
+  w.tok_end = c.mask == SPARSEPR_TOKENS_FULL ? w.ntok : (min(w.row0 + tile_rows, w.rows) - 1) / c.G + 1;
+  w.old_tiles = (w.len + kKeys - 1) / kKeys;
+  w.t_first = part.first * cut.ks;
+  w.t_last = min(part.last * cut.ks, w.old_tiles + (w.tok_end + kKeys - 1) / kKeys);
+  return true;
+}
+
+// The keys of tile i that a row of token `tok` sees, key e in bit e; whether
+// there may be others.
+__device__ __forceinline__ uint32_t seen_keys(const CacheCall& c, const Where& w, const Tree& tree, int i, bool valid, int tok, bool& masked) {
+  masked = true;
+  if (i >= w.old_tiles) {
+    if (!valid) return 0;
+    if (c.mask == SPARSEPR_TOKENS_TREE) return tree.see[tok][i - w.old_tiles];
+    const int k = (c.mask == SPARSEPR_TOKENS_FULL ? w.ntok : tok + 1) - (i - w.old_tiles) * kKeys;
+    return k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1;
+  }
+  const int k = w.len - i * kKeys;
+  masked = k < kKeys;
+  return masked ? (1u << k) - 1 : ~0u;
+}
+
 template <int D, int RS>
 __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_attend(CacheCall c, Cut cut) {
   constexpr int KS = 4 / RS;
@@ -162,31 +213,14 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
   const int n = lane & 31, h = lane >> 5;
   const int rs = wv % RS, ks = wv / RS;
 
-  // Block order: XCD x (block index mod 8) takes the x-th eighth of the parts
-  // in use, the row tiles of a part and head next to each other, which read
-  // the same keys.
-  const int per = part_steps(c, cut, lane);
-  const int64_t used = (int64_t)count_parts(c, cut, per, lane) * c.Hkv * cut.row_tiles;
-  const int64_t eighth = (used + 7) / 8;
-  const int64_t at = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
-  if ((int64_t)(blockIdx.x >> 3) >= eighth || at >= used) return;
-  const int rt = (int)(at % cut.row_tiles), unit = (int)(at / cut.row_tiles);
-  const int hk = unit % c.Hkv, slot = unit / c.Hkv;
-  const Part part = find_part(c, cut, per, slot, lane);
-  if (part.b < 0 || slot >= cut.slots) return;  // (only if lengths change during the launch)
-  const int b = part.b, ntok = cache_count(c, b, c.T), len = cache_length(c, b);
-  const int rows = ntok * c.G, row0 = rt * 32 * RS;
-  if (row0 >= rows) return;
-  // the last token that a row of this tile sees
-  const int tok_end = c.mask == SPARSEPR_TOKENS_FULL ? ntok : (min(row0 + 32 * RS, rows) - 1) / c.G + 1;
-  const int old_tiles = (len + kKeys - 1) / kKeys;
-  const int tiles = old_tiles + (tok_end + kKeys - 1) / kKeys;
-  const int t_first = part.first * KS, t_last = min(part.last * KS, tiles);
-  if (c.mask == SPARSEPR_TOKENS_TREE && t_last > old_tiles) tree_bits(c, b, ntok, tree);
+  Where w;
+  if (!locate(c, cut, 32 * RS, lane, w)) return;
+  if (c.mask == SPARSEPR_TOKENS_TREE && w.t_last > w.old_tiles) tree_bits(c, w.b, w.ntok, tree);
+  const int b = w.b, hk = w.hk, t_first = w.t_first, t_last = w.t_last;
 
   // this lane's row: its B operands, its token
-  const int row = row0 + rs * 32 + n;
-  const bool valid = row < rows;
+  const int row = w.row0 + rs * 32 + n;
+  const bool valid = row < w.rows;
   const int tok = valid ? row / c.G : 0, hq = hk * c.G + (valid ? row % c.G : 0);
   bf16x8 q[NKS];
   {
@@ -217,9 +251,9 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
     cchunk[u] = (uint32_t)(((s % CH) ^ kv_swz<D>(ckey[u])) * 16);
   }
   auto issue = [&](int i, int buf) {
-    const bool old = i < old_tiles;
-    const int key0 = (old ? i : i - old_tiles) * kKeys;
-    const int left = (old ? len : tok_end) - key0 - 1;
+    const bool old = i < w.old_tiles;
+    const int key0 = (old ? i : i - w.old_tiles) * kKeys;
+    const int left = (old ? w.len : w.tok_end) - key0 - 1;
     const int64_t stride = (old ? c.sn : c.nsn) * 2;
     const char* kp = (old ? kc : kn) + key0 * stride;
     const char* vp = (old ? vc : vn) + key0 * stride;
@@ -251,24 +285,8 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
       const bf16x8 kf = __builtin_bit_cast(bf16x8, *(const uint4*)(kt + (n * CH + ((2 * x + h) ^ kv_swz<D>(n))) * 8));
       S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[x], S, 0, 0, 0);
     }
-    // keys that this row does not see: bit e of `see` stands for key e
-    uint32_t see = ~0u;
-    bool masked = false;
-    if (i >= old_tiles) {
-      const int u0 = (i - old_tiles) * kKeys;
-      masked = true;
-      if (!valid)
-        see = 0;
-      else if (c.mask == SPARSEPR_TOKENS_TREE)
-        see = tree.see[tok][i - old_tiles];
-      else {
-        const int k = (c.mask == SPARSEPR_TOKENS_FULL ? ntok : tok + 1) - u0;
-        see = k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1;
-      }
-    } else if (len - i * kKeys < kKeys) {
-      masked = true;
-      see = (1u << (len - i * kKeys)) - 1;
-    }
+    bool masked;
+    const uint32_t see = seen_keys(c, w, tree, i, valid, tok, masked);
     if (masked) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -333,18 +351,18 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
       }
     if (odd) {
       for (int key = 0; key < kKeys; ++key) {
-        float w = 0.f;
+        float pk = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (e == (key >> 3) * 4 + (key & 3)) w = (float)P[e >> 3][e & 7];
-        w = __shfl(w, n + 32 * ((key >> 2) & 1));
+          if (e == (key >> 3) * 4 + (key & 3)) pk = (float)P[e >> 3][e & 7];
+        pk = __shfl(pk, n + 32 * ((key >> 2) & 1));
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int dv = db * 32 + (e >> 2) * 8 + h * 4 + (e & 3);
             const uint16_t x = vt[(key * CH + ((dv >> 3) ^ kv_swz<D>(key))) * 8 + (dv & 7)];
-            if ((x & 0x7f80) == 0x7f80 && !(w == 0.f)) O[db][e] += w * bf16_bits_to_f32(x);
+            if ((x & 0x7f80) == 0x7f80 && !(pk == 0.f)) O[db][e] += pk * bf16_bits_to_f32(x);
           }
       }
     }
@@ -407,8 +425,8 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
     }
   }
   if (!valid) return;
-  if (part.count > 1) {
-    const size_t at_row = ((size_t)slot * c.Hkv + hk) * ((size_t)c.T * c.G) + row;
+  if (w.parts > 1) {
+    const size_t at_row = ((size_t)w.slot * c.Hkv + hk) * ((size_t)c.T * c.G) + row;
     float* dst = cut.o + at_row * D;
     if (h == 0) cut.ml[at_row] = make_float2(m_run, l_tot);
 #pragma unroll
@@ -434,6 +452,195 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
       *(uint2*)(dst + db * 32 + (e >> 2) * 8 + h * 4) = make_uint2(o[0], o[1]);
     }
   if (h == 0 && c.lse) c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok] = (m_run + log2f(l_tot)) * 0.6931471805599453f;
+}
+
+// The same for fp32 on v_mfma_f32_32x32x2_f32.  Both contractions may take
+// their terms in any order: lane (n, h) holds dims 8 j + 4 h + 0..3 of row n, so
+// that a 16-byte load of a key feeds four products, and the V product's step e
+// contracts the keys of score register e of both halves, V^T row m of block db
+// being channel m NDB + db, so that one load of a value row serves all blocks.
+// Operands go straight from memory to registers: a load feeds 256 matrix
+// cycles, so four waves ask for at most 16 bytes a clock.
+template <int D, int RS>
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(CacheCall c, Cut cut) {
+  constexpr int KS = 4 / RS;
+  constexpr int NQ = D / 8, HQ = NQ / 2, NDB = D / 32, NREG = 16 * NDB;
+  typedef float fv __attribute__((ext_vector_type(NDB)));
+  __shared__ float red[KS > 1 ? (KS - 1) * RS : 1][NREG + 2][64];
+  __shared__ Tree tree;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, h = lane >> 5;
+  const int rs = wv % RS, ks = wv / RS;
+  Where w;
+  if (!locate(c, cut, 32 * RS, lane, w)) return;
+  if (c.mask == SPARSEPR_TOKENS_TREE && w.t_last > w.old_tiles) tree_bits(c, w.b, w.ntok, tree);
+  const int b = w.b, hk = w.hk;
+  const int row = w.row0 + rs * 32 + n;
+  const bool valid = row < w.rows;
+  const int tok = valid ? row / c.G : 0, hq = hk * c.G + (valid ? row % c.G : 0);
+  f32x4 q[NQ];
+  {
+    const float* src = (const float*)c.q + b * c.qsb + hq * c.qsh + tok * c.qsn + 4 * h;
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) q[j] = *(const f32x4*)(src + 8 * j);
+  }
+  const float* kc = (const float*)c.k + b * c.sb + hk * c.sh;
+  const float* vc = (const float*)c.v + b * c.sb + hk * c.sh;
+  const float* kn = (const float*)c.kn + b * c.nsb + hk * c.nsh;
+  const float* vn = (const float*)c.vn + b * c.nsb + hk * c.nsh;
+  // memory row of key x of tile i; rows past the end repeat the last one
+  auto key_at = [&](int i, int x) {
+    return i < w.old_tiles ? min(i * kKeys + x, w.len - 1) : min((i - w.old_tiles) * kKeys + x, w.tok_end - 1);
+  };
+  f32x4 ka[HQ], kb[HQ];
+  fv va[8], vb[8];
+  auto load_k = [&](f32x4* dst, int i, int half) {
+    const bool old = i < w.old_tiles;
+    const float* src = (old ? kc : kn) + key_at(i, n) * (old ? c.sn : c.nsn) + 4 * h + half * (HQ * 8);
+#pragma unroll
+    for (int j = 0; j < HQ; ++j) dst[j] = *(const f32x4*)(src + 8 * j);
+  };
+  auto load_v = [&](fv* dst, int i, int half) {
+    const bool old = i < w.old_tiles;
+    const float* src = (old ? vc : vn) + n * NDB;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      dst[e] = *(const fv*)(src + key_at(i, half * 16 + (e >> 2) * 8 + 4 * h + (e & 3)) * (old ? c.sn : c.nsn));
+  };
+  const float sl2 = 1.4426950408889634f / sqrtf((float)D);
+  float m_run = kNoMax, l_run = 0.f;
+  f32x16 S, O[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) O[db][e] = 0.f;
+  auto scores = [&](const f32x4* kk, int half) {
+#pragma unroll
+    for (int j = 0; j < HQ; ++j)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) S = __builtin_amdgcn_mfma_f32_32x32x2f32(kk[j][x], q[half * HQ + j][x], S, 0, 0, 0);
+  };
+  auto pv = [&](const fv* vv, int half) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+        O[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv[e][db], S[half * 8 + e], O[db], 0, 0, 0);
+  };
+  int i = w.t_first + ks;
+  if (i < w.t_last) load_k(ka, i, 0);
+  for (; i < w.t_last; i += KS) {
+    load_k(kb, i, 1);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) S[e] = 0.f;
+    scores(ka, 0);
+    load_v(va, i, 0);
+    scores(kb, 1);
+    load_v(vb, i, 1);
+    bool masked;
+    const uint32_t see = seen_keys(c, w, tree, i, valid, tok, masked);
+    if (masked) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!((see >> ((e >> 2) * 8 + h * 4 + (e & 3))) & 1)) S[e] = -INFINITY;
+    }
+    float mt = fmaxf(fmaxf(S[0], S[1]), S[2]);
+#pragma unroll
+    for (int e = 3; e < 15; e += 2) mt = fmaxf(fmaxf(mt, S[e]), S[e + 1]);
+    const float mp = pair_max(fmaxf(mt, S[15])) * sl2;
+    if (__any(mp > m_run)) {
+      const float m_new = fmaxf(m_run, mp);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) O[db][e] *= alpha;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f(fmaf(S[e], sl2, -m_run));
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) l_run += (S[e] + S[e + 1]) + (S[e + 2] + S[e + 3]);
+    // infinite and NaN values of masked keys, as in the bf16 kernel
+    if (masked) {
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) any |= !__builtin_isfinite(va[e][db]) || !__builtin_isfinite(vb[e][db]);
+      if (__ballot(any)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) {
+            if (!__builtin_isfinite(va[e][db])) va[e][db] = 0.f;
+            if (!__builtin_isfinite(vb[e][db])) vb[e][db] = 0.f;
+          }
+        const bool old = i < w.old_tiles;
+        for (int key = 0; key < kKeys; ++key) {
+          float pk = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (e == (key >> 3) * 4 + (key & 3)) pk = S[e];
+          pk = __shfl(pk, n + 32 * ((key >> 2) & 1));
+          const float* src = (old ? vc : vn) + key_at(i, key) * (old ? c.sn : c.nsn);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) {
+              const float x = src[((e >> 2) * 8 + 4 * h + (e & 3)) * NDB + db];
+              if (!__builtin_isfinite(x) && !(pk == 0.f)) O[db][e] += pk * x;
+            }
+        }
+      }
+    }
+    pv(va, 0);
+    if (i + KS < w.t_last) load_k(ka, i + KS, 0);
+    pv(vb, 1);
+  }
+  float l_tot = pair_sum(l_run);
+  if (KS > 1) {
+    if (ks > 0) {
+      float(*dst)[64] = red[(ks - 1) * RS + rs];
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dst[db * 16 + e][lane] = O[db][e];
+      dst[NREG][lane] = m_run;
+      dst[NREG + 1][lane] = l_tot;
+    }
+    __syncthreads();
+    if (ks > 0) return;
+    for (int x = 1; x < KS; ++x) {
+      const float(*src)[64] = red[(x - 1) * RS + rs];
+      const float mp = src[NREG][lane], lp = src[NREG + 1][lane];
+      const float m_new = fmaxf(m_run, mp);
+      const float fa = __builtin_amdgcn_exp2f(m_run - m_new), fb = __builtin_amdgcn_exp2f(mp - m_new);
+      m_run = m_new;
+      l_tot = l_tot * fa + lp * fb;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) O[db][e] = O[db][e] * fa + src[db * 16 + e][lane] * fb;
+    }
+  }
+  if (!valid) return;
+  const size_t at_row = ((size_t)w.slot * c.Hkv + hk) * ((size_t)c.T * c.G) + row;
+  float* dst = w.parts > 1 ? cut.o + at_row * D : (float*)c.out + b * c.osb + hq * c.osh + tok * c.osn;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    fv o;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) o[db] = w.parts > 1 ? O[db][e] : O[db][e] / l_tot;
+    *(fv*)(dst + ((e >> 2) * 8 + 4 * h + (e & 3)) * NDB) = o;
+  }
+  if (h > 0) return;
+  if (w.parts > 1)
+    cut.ml[at_row] = make_float2(m_run, l_tot);
+  else if (c.lse)
+    c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok] = (m_run + log2f(l_tot)) * 0.6931471805599453f;
 }
 
 // Join the parts of the rows whose keys were split: one block a row, its
@@ -522,29 +729,39 @@ Cut make_cut(const CacheCall& c) {
 size_t rows_of(const CacheCall& c, const Cut& cut) { return (size_t)cut.slots * c.Hkv * c.T * c.G; }
 
 template <int D>
-void attend_bf16(const CacheCall& c, const Cut& cut, hipStream_t s) {
+void attend(const CacheCall& c, const Cut& cut, hipStream_t s) {
   const int64_t blocks = ((int64_t)cut.slots * c.Hkv * cut.row_tiles + 7) / 8 * 8;
-  const dim3 grid((unsigned)blocks);
+  const dim3 grid((unsigned)blocks), rows((unsigned)(c.B * c.Hkv * c.T * c.G));
+  auto sets = [&](auto rs) {
+    if (c.bf16)
+      k_cache_attend<D, rs.value><<<grid, 256, 0, s>>>(c, cut);
+    else
+      k_cache_attend_f32<D, rs.value><<<grid, 256, 0, s>>>(c, cut);
+  };
   switch (row_sets(c)) {
-    case 1: k_cache_attend<D, 1><<<grid, 256, 0, s>>>(c, cut); break;
-    case 2: k_cache_attend<D, 2><<<grid, 256, 0, s>>>(c, cut); break;
-    default: k_cache_attend<D, 4><<<grid, 256, 0, s>>>(c, cut);
+    case 1: sets(std::integral_constant<int, 1>{}); break;
+    case 2: sets(std::integral_constant<int, 2>{}); break;
+    default: sets(std::integral_constant<int, 4>{});
   }
-  if (cut.split) k_cache_join<D, 1><<<(unsigned)(c.B * c.Hkv * c.T * c.G), 256, 0, s>>>(c, cut);
+  if (!cut.split) return;
+  if (c.bf16)
+    k_cache_join<D, 1><<<rows, 256, 0, s>>>(c, cut);
+  else
+    k_cache_join<D, 0><<<rows, 256, 0, s>>>(c, cut);
 }
 
 }  // namespace
 
-size_t cache_attend_workspace_bf16(const CacheCall& c) {
+size_t cache_attend_workspace(const CacheCall& c) {
   const Cut cut = make_cut(c);
   return cut.split ? rows_of(c, cut) * (c.d * 4 + 8) : 0;
 }
 
-void launch_cache_attend_bf16(const CacheCall& c, void* ws, hipStream_t s) {
+void launch_cache_attend(const CacheCall& c, void* ws, hipStream_t s) {
   Cut cut = make_cut(c);
   cut.o = (float*)ws;
   cut.ml = (float2*)(cut.o + rows_of(c, cut) * c.d);
-  c.d == 64 ? attend_bf16<64>(c, cut, s) : attend_bf16<128>(c, cut, s);
+  c.d == 64 ? attend<64>(c, cut, s) : attend<128>(c, cut, s);
 }
 
 }  // namespace sparsepr

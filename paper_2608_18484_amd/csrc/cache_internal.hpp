@@ -40,8 +40,6 @@ struct CacheCall {
 
 size_t cache_attend_workspace(const CacheCall& c);
 void launch_cache_attend(const CacheCall& c, void* ws, hipStream_t s);
-size_t cache_attend_workspace_bf16(const CacheCall& c);
-void launch_cache_attend_bf16(const CacheCall& c, void* ws, hipStream_t s);
 
 void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int32_t* lengths_out,
                          hipStream_t s);

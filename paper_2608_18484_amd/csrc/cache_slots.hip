@@ -1,91 +1,14 @@
-// Kernels of the operators on a K/V cache for gfx950: attention of new tokens,
-// append, eviction (cache_attn.hip and cache_weigh.hip have the products on the
-// matrix cores).
+// Append and eviction on a K/V cache for gfx950.
 #include <hip/hip_runtime.h>
-#include <float.h>
 #include <limits.h>
-#include <math.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "cache_device.hpp"
 
 namespace sparsepr {
 
 namespace {
-
-constexpr float kNoMax = -FLT_MAX;
-
-// ---- attention --------------------------------------------------------------
-
-// Whether token t sees token u (u < T).
-__device__ __forceinline__ bool token_sees(const CacheCall& c, const int32_t* par, int t, int u) {
-  if (c.mask == SPARSEPR_TOKENS_FULL) return true;
-  if (c.mask == SPARSEPR_TOKENS_CAUSAL) return u <= t;
-  while (t > u) {
-    const int p = par[t];
-    t = p < -1 || p >= t ? -1 : p;
-  }
-  return t == u;
-}
-
-// One block a row: every thread runs an online softmax over each 256th key in
-// registers, the threads' parts are joined at the end.
-template <int D>
-__global__ __launch_bounds__(256) void k_cache_attend_f32(CacheCall c) {
-  constexpr int BF16 = 0;
-  __shared__ float red[4][D + 2];
-  const int H = c.Hkv * c.G, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const int t = blockIdx.x % c.T, bh = blockIdx.x / c.T, b = bh / H, hq = bh % H, hk = hq / c.G;
-  const int n = cache_count(c, b, c.T), len = cache_length(c, b);
-  if (t >= n) return;
-  const int32_t* par = c.parents ? c.parents + (size_t)b * c.T : nullptr;
-  if (par && tid == 0 && (par[t] < -1 || par[t] >= t)) raise_flag(c, b, SPARSEPR_CACHE_FLAG_BAD_INDEX);
-  const int64_t qo = b * c.qsb + hq * c.qsh + t * c.qsn;
-  float m = kNoMax, l = 0.f, O[D];
-#pragma unroll
-  for (int i = 0; i < D; ++i) O[i] = 0.f;
-  const float scale = 1.f / sqrtf((float)D);
-  for (int j = tid; j < len + n; j += 256) {
-    const void *kp = c.k, *vp = c.v;
-    int64_t o = b * c.sb + hk * c.sh + (int64_t)j * c.sn;
-    if (j >= len) {
-      if (!token_sees(c, par, t, j - len)) continue;
-      kp = c.kn;
-      vp = c.vn;
-      o = b * c.nsb + hk * c.nsh + (int64_t)(j - len) * c.nsn;
-    }
-    float s = 0.f;
-    for (int i = 0; i < D; ++i) s = fmaf(load_x(c.q, BF16, qo + i), load_x(kp, BF16, o + i), s);
-    s *= scale;
-    const float mn = fmaxf(m, s), a = expf(m - mn), p = expf(s - mn);
-    m = mn;
-    l = l * a + p;
-#pragma unroll
-    for (int i = 0; i < D; ++i) O[i] = fmaf(p, load_x(vp, BF16, o + i), O[i] * a);
-  }
-  const float mw = wave_max(m), a = expf(m - mw);
-  l = wave_sum(l * a);
-#pragma unroll
-  for (int i = 0; i < D; ++i) {
-    const float o = wave_sum(O[i] * a);
-    if (lane == 0) red[wv][i] = o;
-  }
-  if (lane == 0) red[wv][D] = mw, red[wv][D + 1] = l;
-  __syncthreads();
-  if (tid >= D) return;
-  m = fmaxf(fmaxf(red[0][D], red[1][D]), fmaxf(red[2][D], red[3][D]));
-  float o = 0.f;
-  l = 0.f;
-  for (int w = 0; w < 4; ++w) {
-    const float f = expf(red[w][D] - m);
-    l += red[w][D + 1] * f;
-    o += red[w][tid] * f;
-  }
-  ((float*)c.out)[b * c.osb + hq * c.osh + t * c.osn + tid] = o / l;
-  if (tid == 0 && c.lse) c.lse[((size_t)b * H + hq) * c.T + t] = m + logf(l);
-}
 
 // ---- append -----------------------------------------------------------------
 
@@ -268,18 +191,6 @@ EvictWork evict_work(const CacheCall& c, int budget, void* ws) {
 }
 
 }  // namespace
-
-size_t cache_attend_workspace(const CacheCall& c) { return c.bf16 ? cache_attend_workspace_bf16(c) : 0; }
-
-void launch_cache_attend(const CacheCall& c, void* ws, hipStream_t s) {
-  const unsigned rows = (unsigned)(c.B * c.Hkv * c.G * c.T);
-  if (c.bf16)
-    launch_cache_attend_bf16(c, ws, s);
-  else if (c.d == 64)
-    k_cache_attend_f32<64><<<rows, 256, 0, s>>>(c);
-  else
-    k_cache_attend_f32<128><<<rows, 256, 0, s>>>(c);
-}
 
 void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int32_t* lengths_out,
                          hipStream_t s) {

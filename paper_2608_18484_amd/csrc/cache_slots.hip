@@ -3,6 +3,7 @@
 #include <limits.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache_device.hpp"
 
@@ -63,102 +64,180 @@ __global__ __launch_bounds__(256) void k_cache_append_lengths(CacheCall c) {
 
 // ---- eviction ---------------------------------------------------------------
 
-// Workspace of an eviction: per K/V head the kept slots' sources src[budget],
-// the freed slots hole[budget], and (rows to move, rows kept).
+// Workspace of an eviction: per K/V head (rows to move, rows kept), the freed
+// slots and the slots that move into them, and for another cache the source of
+// every kept slot.
 struct EvictWork {
-  int32_t* src;
-  int32_t* hole;
   int2* count;
+  int32_t* hole;   // [budget]
+  int32_t* mover;  // [budget]
+  int32_t* src;    // [budget]
 };
 
-__device__ __forceinline__ uint32_t evict_key(const CacheCall& c, size_t base, int j, int n_sink, int n_recent, int newest) {
-  if (n_sink > 0 || n_recent > 0) {
-    const int p = c.positions[base + j];
-    if (p < n_sink || (n_recent > 0 && (int64_t)p > (int64_t)newest - n_recent)) return 0xffffffffu;
-  }
-  const float f = c.scores[base + j] + 0.f;  // -0 ranks with 0
+__device__ __forceinline__ uint32_t evict_key(float score, int pos, bool by_pos, int n_sink, int n_recent, int newest) {
+  if (by_pos && (pos < n_sink || (n_recent > 0 && (int64_t)pos > (int64_t)newest - n_recent))) return 0xffffffffu;
+  const float f = score + 0.f;  // -0 ranks with 0
   return f != f ? 0xfffffffeu : float_order_bits(f);
 }
 
 // One block a K/V head: the budget-th largest key by four 8-bit digits, then
-// one pass over the slots in order that numbers the freed and the moving ones.
-__global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w, int budget, int n_sink, int n_recent) {
-  __shared__ int hist[256];
-  __shared__ int wsum[3][16], sh_digit, sh_need, sh_newest;
-  const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+// the freed and the moving slots numbered in their order.
+//
+// Each of the 16 waves has a run of neighbouring slots, 64 at a time, and keeps
+// their keys in registers (PER of them a lane; PER = 0: read again for every
+// pass), so that the digits' passes read no memory and the numbering needs one
+// exchange between the waves, not one for every 1,024 slots.
+template <int PER>
+__global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w, int in_place, int budget, int n_sink, int n_recent) {
+  constexpr int COPIES = 4;  // of the histogram: lanes of equal digits meet less
+  __shared__ int hist[256][COPIES];
+  __shared__ int wsum[3][16], sh_digit, sh_need, sh_same, sh_newest;
+  const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = cache_length(c, bh / c.Hkv);
-  const size_t base = (size_t)bh * c.cap;
-  int32_t* src = w.src + (size_t)bh * budget;
+  const float* score = c.scores + (size_t)bh * c.cap;
+  const bool by_pos = n_sink > 0 || n_recent > 0;
+  const int32_t* pos = by_pos ? c.positions + (size_t)bh * c.cap : nullptr;
   int32_t* hole = w.hole + (size_t)bh * budget;
+  int32_t* mover = w.mover + (size_t)bh * budget;
+  int32_t* src = w.src + (size_t)bh * budget;
   if (len <= budget) {
-    for (int j = tid; j < len; j += 1024) src[j] = j;
+    if (!in_place)
+      for (int j = tid; j < len; j += 1024) src[j] = j;
     if (tid == 0) w.count[bh] = make_int2(0, len);
     return;
   }
+  const int turns = (len + 1023) / 1024;  // of a wave, 64 slots each
+  const int j0 = wv * turns * 64 + lane;
   if (tid == 0) sh_newest = INT_MIN;
   __syncthreads();
   if (n_recent > 0) {
     int m = INT_MIN;
-    for (int j = tid; j < len; j += 1024) m = max(m, c.positions[base + j]);
-    atomicMax(&sh_newest, m);
+#pragma unroll 8
+    for (int i = 0; i < turns; ++i) m = max(m, pos[min(j0 + i * 64, len - 1)]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o));
+    if (lane == 0) atomicMax(&sh_newest, m);
     __syncthreads();
   }
   const int newest = sh_newest;
+  // slots past the end rank below every number (whose keys are at least that
+  // of -inf), so that only `len` tells them apart
+  auto load = [&](int i) {
+    const int j = j0 + i * 64, x = min(j, len - 1);
+    const uint32_t k = evict_key(score[x], by_pos ? pos[x] : 0, by_pos, n_sink, n_recent, newest);
+    return j < len ? k : 0u;
+  };
+  uint32_t key[PER ? PER : 1];
+  if (PER) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = i < turns ? load(i) : 0;
+  }
+  // f(turn, key) for this lane's slots in order; every lane of a wave takes part
+  auto each = [&](auto&& f) {
+    if (PER) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (i < turns) f(i, key[i]);
+    } else {
+      for (int i = 0; i < turns; i += 8) {
+        uint32_t k[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) k[x] = load(i + x);
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          if (i + x < turns) f(i + x, k[x]);
+      }
+    }
+  };
   uint32_t prefix = 0, mask = 0;
   int need = budget;  // keys still to take among those that match the prefix
   for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
+    (&hist[0][0])[tid] = 0;
     __syncthreads();
-    for (int j = tid; j < len; j += 1024) {
-      const uint32_t k = evict_key(c, base, j, n_sink, n_recent, newest);
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
-    }
+    each([&](int, uint32_t k) {
+      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255][lane & (COPIES - 1)], 1);
+    });
     __syncthreads();
-    if (tid == 0) {
-      int d = 255, left = need;
-      while (hist[d] < left) left -= hist[d--];
-      sh_digit = d;
-      sh_need = left;
+    if (wv == 0) {
+      // lane x has the digits 255 - 4 x and down; the one where the sum from the
+      // top reaches `need` is the next of the prefix
+      int n[4], own = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int4 h = *(const int4*)hist[255 - 4 * lane - e];
+        n[e] = h.x + h.y + h.z + h.w;
+        own += n[e];
+      }
+      int upto = own;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(upto, o);
+        if (lane >= o) upto += y;
+      }
+      if (upto >= need && upto - own < need) {
+        int left = need - (upto - own), e = 0;
+        while (n[e] < left) left -= n[e++];
+        sh_digit = 255 - 4 * lane - e;
+        sh_need = left;
+        sh_same = n[e];
+      }
     }
     __syncthreads();
     need = sh_need;
     prefix |= (uint32_t)sh_digit << shift;
     mask |= 255u << shift;
-    __syncthreads();
   }
   // keys above `prefix` stay, and the first `need` that equal it
-  int n_eq = 0, n_hole = 0, n_move = 0;
-  for (int j0 = 0; j0 < len; j0 += 1024) {
-    const int j = j0 + tid;
-    const bool in = j < len;
-    const uint32_t k = in ? evict_key(c, base, j, n_sink, n_recent, newest) : 0;
-    const bool eq = in && k == prefix;
-    const uint64_t before = lane ? ~0ull >> (64 - lane) : 0;
-    const uint64_t beq = __ballot(eq);
-    if (lane == 0) wsum[0][wv] = __popcll(beq);
+  const uint64_t before = lane ? ~0ull >> (64 - lane) : 0;
+  int n_hole = 0, n_move = 0, eq0 = 0;
+  const bool ties = sh_same > need;
+  if (ties) {
+    int n_eq = 0;
+    each([&](int, uint32_t k) { n_eq += __popcll(__ballot(k == prefix)); });
+    if (lane == 0) wsum[0][wv] = n_eq;
     __syncthreads();
-    int req = n_eq + __popcll(beq & before);
-    for (int x = 0; x < 16; ++x) {
-      if (x < wv) req += wsum[0][x];
-      n_eq += wsum[0][x];
-    }
-    const bool keep = in && (k > prefix || (eq && req < need));
-    const bool ho = in && j < budget && !keep, mv = keep && j >= budget;
-    const uint64_t bho = __ballot(ho), bmv = __ballot(mv);
-    if (lane == 0) wsum[1][wv] = __popcll(bho), wsum[2][wv] = __popcll(bmv);
-    __syncthreads();
-    int rho = n_hole + __popcll(bho & before), rmv = n_move + __popcll(bmv & before);
-    for (int x = 0; x < 16; ++x) {
-      if (x < wv) rho += wsum[1][x], rmv += wsum[2][x];
-      n_hole += wsum[1][x];
-      n_move += wsum[2][x];
-    }
-    if (keep && j < budget) src[j] = j;
-    if (ho) hole[rho] = j;
-    __syncthreads();
-    if (mv) src[hole[rmv]] = j;
+    for (int x = 0; x < wv; ++x) eq0 += wsum[0][x];
   }
-  if (tid == 0) w.count[bh] = make_int2(n_move, budget);
+  // f(slot, freed, moves, ballots of both) in the slots' order
+  auto number = [&](auto&& f) {
+    int eq = eq0, bud = budget;
+    asm volatile("" : "+s"(bud));  // (keeps the comparisons with it out of registers between the passes)
+    each([&](int i, uint32_t k) {
+      const int j = j0 + i * 64;
+      bool keep = k >= prefix;
+      if (ties) {
+        const uint64_t beq = __ballot(k == prefix);
+        keep = k > prefix || (k == prefix && eq + __popcll(beq & before) < need);
+        eq += __popcll(beq);
+      }
+      const bool freed = j < bud && !keep, moves = keep && j >= bud;
+      f(j, freed, moves, __ballot(freed), __ballot(moves));
+    });
+  };
+  number([&](int, bool, bool, uint64_t bf, uint64_t bm) {
+    n_hole += __popcll(bf);
+    n_move += __popcll(bm);
+  });
+  if (lane == 0) wsum[1][wv] = n_hole, wsum[2][wv] = n_move;
+  __syncthreads();
+  int at_hole = 0, at_move = 0, moves_all = 0;
+  for (int x = 0; x < 16; ++x) {
+    if (x < wv) at_hole += wsum[1][x], at_move += wsum[2][x];
+    moves_all += wsum[2][x];
+  }
+  number([&](int j, bool freed, bool moves, uint64_t bf, uint64_t bm) {
+    if (freed) hole[at_hole + __popcll(bf & before)] = j;
+    if (moves) mover[at_move + __popcll(bm & before)] = j;
+    if (!in_place && !freed && j < budget) src[j] = j;
+    at_hole += __popcll(bf);
+    at_move += __popcll(bm);
+  });
+  if (!in_place) {
+    __syncthreads();
+    for (int r = tid; r < moves_all; r += 1024) src[hole[r]] = mover[r];
+  }
+  if (tid == 0) w.count[bh] = make_int2(moves_all, budget);
 }
 
 // The kept rows to their slots, 16 bytes of K and of V a thread.
@@ -171,7 +250,7 @@ __global__ __launch_bounds__(256) void k_evict_move(CacheCall c, EvictTo to, Evi
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * ch; i += (int64_t)gridDim.x * 256) {
     const int r = (int)(i / ch), part = (int)(i % ch);
     const int dst = to.in_place ? w.hole[(size_t)bh * budget + r] : r;
-    const int src = w.src[(size_t)bh * budget + dst];
+    const int src = (to.in_place ? w.mover : w.src)[(size_t)bh * budget + r];
     const int64_t so = (b * c.sb + hk * c.sh + (int64_t)src * c.sn) * es + part * 16;
     const int64_t po = (b * to.sb + hk * to.sh + (int64_t)dst * to.sn) * es + part * 16;
     const uint4 kv = *(const uint4*)((const char*)c.k + so), vv = *(const uint4*)((const char*)c.v + so);
@@ -186,8 +265,9 @@ __global__ __launch_bounds__(256) void k_evict_move(CacheCall c, EvictTo to, Evi
 
 EvictWork evict_work(const CacheCall& c, int budget, void* ws) {
   const size_t n = (size_t)c.B * c.Hkv;
-  char* p = (char*)ws;
-  return {(int32_t*)(p + n * 8), (int32_t*)(p + n * 8) + n * budget, (int2*)p};
+  int2* count = (int2*)ws;
+  int32_t* p = (int32_t*)(count + n);
+  return {count, p, p + n * budget, p + 2 * n * budget};
 }
 
 }  // namespace
@@ -201,13 +281,23 @@ void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int
 }
 
 size_t cache_evict_workspace(const CacheCall& c, int budget) {
-  return (size_t)c.B * c.Hkv * (8 + 8 * (size_t)budget);
+  return (size_t)c.B * c.Hkv * (8 + 12 * (size_t)budget);
 }
 
 void launch_cache_evict(const CacheCall& c, const EvictTo& to, int budget, int n_sink,
                         int n_recent, void* ws, hipStream_t s) {
   const EvictWork w = evict_work(c, budget, ws);
-  k_evict_select<<<c.B * c.Hkv, 1024, 0, s>>>(c, w, budget, n_sink, n_recent);
+  auto select = [&](auto per) {
+    k_evict_select<per.value><<<c.B * c.Hkv, 1024, 0, s>>>(c, w, to.in_place, budget, n_sink, n_recent);
+  };
+  if (c.cap <= 8 * 1024)
+    select(std::integral_constant<int, 8>{});
+  else if (c.cap <= 32 * 1024)
+    select(std::integral_constant<int, 32>{});
+  else if (c.cap <= 80 * 1024)
+    select(std::integral_constant<int, 80>{});
+  else
+    select(std::integral_constant<int, 0>{});
   const int ch = c.d * (c.bf16 ? 2 : 4) / 16;
   const int64_t most = to.in_place ? std::min(budget, std::max(c.cap - budget, 1)) : budget;
   const unsigned blocks = (unsigned)std::min<int64_t>((most * ch + 255) / 256, 256);

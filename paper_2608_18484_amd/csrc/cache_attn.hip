@@ -142,15 +142,19 @@ __device__ __forceinline__ void wait_copies() {  // at most N of this wave's cop
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-__device__ __forceinline__ uint32_t odd_bf16(uint32_t x) {  // either half infinite or NaN
-  return (uint32_t)((x & 0x7f80u) == 0x7f80u) | (uint32_t)((x & 0x7f800000u) == 0x7f800000u);
+// Two bf16 values, 0 in the place of one that is infinite or NaN.
+__device__ __forceinline__ uint32_t finite_bf16(uint32_t x) {
+  if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+  if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+  return x;
 }
 
 // What a block works on.
 struct Where {
   int slot, hk, b, parts;     // part, K/V head, entry, the entry's parts
   int ntok, len, rows, row0;  // the entry's tokens, slots and rows; the tile's first row
-  int tok_end, old_tiles;     // tokens that its rows see at most; tiles of the slots
+  int tok_end;                // tokens that its rows see at most
+  int full_tiles, old_tiles;  // tiles of 32 slots in use; tiles of the slots
   int t_first, t_last;        // key tiles
 };
 
@@ -176,25 +180,20 @@ __device__ __forceinline__ bool locate(const CacheCall& c, const Cut& cut, int t
   w.row0 = rt * tile_rows;
   if (w.row0 >= w.rows) return false;
   w.tok_end = c.mask == SPARSEPR_TOKENS_FULL ? w.ntok : (min(w.row0 + tile_rows, w.rows) - 1) / c.G + 1;
+  w.full_tiles = w.len / kKeys;
   w.old_tiles = (w.len + kKeys - 1) / kKeys;
   w.t_first = part.first * cut.ks;
   w.t_last = min(part.last * cut.ks, w.old_tiles + (w.tok_end + kKeys - 1) / kKeys);
   return true;
 }
 
-// The keys of tile i that a row of token `tok` sees, key e in bit e; whether
-// there may be others.
-__device__ __forceinline__ uint32_t seen_keys(const CacheCall& c, const Where& w, const Tree& tree, int i, bool valid, int tok, bool& masked) {
-  masked = true;
-  if (i >= w.old_tiles) {
-    if (!valid) return 0;
-    if (c.mask == SPARSEPR_TOKENS_TREE) return tree.see[tok][i - w.old_tiles];
-    const int k = (c.mask == SPARSEPR_TOKENS_FULL ? w.ntok : tok + 1) - (i - w.old_tiles) * kKeys;
-    return k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1;
-  }
-  const int k = w.len - i * kKeys;
-  masked = k < kKeys;
-  return masked ? (1u << k) - 1 : ~0u;
+// The keys of tile i >= full_tiles that a row of token `tok` sees, key e in bit e.
+__device__ __forceinline__ uint32_t seen_keys(const CacheCall& c, const Where& w, const Tree& tree, int i, bool valid, int tok) {
+  if (i < w.old_tiles) return (1u << (w.len - i * kKeys)) - 1;
+  if (!valid) return 0;
+  if (c.mask == SPARSEPR_TOKENS_TREE) return tree.see[tok][i - w.old_tiles];
+  const int k = (c.mask == SPARSEPR_TOKENS_FULL ? w.ntok : tok + 1) - (i - w.old_tiles) * kKeys;
+  return k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1;
 }
 
 template <int D, int RS>
@@ -241,29 +240,34 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
     return __builtin_amdgcn_readfirstlane(
         (uint32_t)(size_t)(const __attribute__((address_space(3))) void*)p);
   };
-  // copies of this wave's share of key tile i; rows past the end repeat the last one
+  // copies of this wave's share of one of key tile i's tensors (0 = K, 1 = V);
+  // rows past the end repeat the last one
   int ckey[CPW];
-  uint32_t cchunk[CPW];
+  uint32_t cchunk[CPW], voff[CPW];
 #pragma unroll
   for (int u = 0; u < CPW; ++u) {
     const int s = (u * RS + rs) * 64 + lane;
     ckey[u] = s / CH;
     cchunk[u] = (uint32_t)(((s % CH) ^ kv_swz<D>(ckey[u])) * 16);
+    voff[u] = (uint32_t)ckey[u] * (uint32_t)(c.sn * 2) + cchunk[u];
   }
-  auto issue = [&](int i, int buf) {
+  const uint32_t kv_lds = lds_of(&kv[ks][0][0][0]) + rs * 1024;
+  auto issue = [&](int i, int which, int buf) {
+    const uint32_t dst = kv_lds + (uint32_t)(buf * 2 + which) * (TE * 2);
+    if (i < w.full_tiles) {
+      const char* p = (which ? vc : kc) + (int64_t)i * (c.sn * (2 * kKeys));
+#pragma unroll
+      for (int u = 0; u < CPW; ++u) g2lds16s(p, voff[u], dst + u * RS * 1024);
+      return;
+    }
     const bool old = i < w.old_tiles;
     const int key0 = (old ? i : i - w.old_tiles) * kKeys;
     const int left = (old ? w.len : w.tok_end) - key0 - 1;
     const int64_t stride = (old ? c.sn : c.nsn) * 2;
-    const char* kp = (old ? kc : kn) + key0 * stride;
-    const char* vp = (old ? vc : vn) + key0 * stride;
-    const uint32_t kd = lds_of(&kv[ks][buf][0][0]), vd = lds_of(&kv[ks][buf][1][0]);
+    const char* p = (which ? (old ? vc : vn) : (old ? kc : kn)) + key0 * stride;
 #pragma unroll
     for (int u = 0; u < CPW; ++u)
-      g2lds16s(kp, (uint32_t)min(ckey[u], left) * (uint32_t)stride + cchunk[u], kd + (u * RS + rs) * 1024);
-#pragma unroll
-    for (int u = 0; u < CPW; ++u)
-      g2lds16s(vp, (uint32_t)min(ckey[u], left) * (uint32_t)stride + cchunk[u], vd + (u * RS + rs) * 1024);
+      g2lds16s(p, (uint32_t)min(ckey[u], left) * (uint32_t)stride + cchunk[u], dst + u * RS * 1024);
   };
 
   const float sl2 = 1.4426950408889634f / sqrtf((float)D);
@@ -274,10 +278,8 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
 #pragma unroll
     for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
 
-  auto compute = [&](int i, int buf) {
+  auto scores = [&](f32x16& S, int buf) {
     const uint16_t* kt = kv[ks][buf][0];
-    const uint16_t* vt = kv[ks][buf][1];
-    f32x16 S;
 #pragma unroll
     for (int e = 0; e < 16; ++e) S[e] = 0.f;
 #pragma unroll
@@ -285,9 +287,12 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
       const bf16x8 kf = __builtin_bit_cast(bf16x8, *(const uint4*)(kt + (n * CH + ((2 * x + h) ^ kv_swz<D>(n))) * 8));
       S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[x], S, 0, 0, 0);
     }
-    bool masked;
-    const uint32_t see = seen_keys(c, w, tree, i, valid, tok, masked);
-    if (masked) {
+  };
+  // the scores of the keys that this row does not see become -inf; the maximum
+  // of the lane's others
+  auto mask_max = [&](f32x16& S, int i) {
+    if (i >= w.full_tiles) {
+      const uint32_t see = seen_keys(c, w, tree, i, valid, tok);
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (!((see >> ((e >> 2) * 8 + h * 4 + (e & 3))) & 1)) S[e] = -INFINITY;
@@ -295,7 +300,30 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
     float mt = fmaxf(fmaxf(S[0], S[1]), S[2]);
 #pragma unroll
     for (int e = 3; e < 15; e += 2) mt = fmaxf(fmaxf(mt, S[e]), S[e + 1]);
-    const float mp = pair_max(fmaxf(mt, S[15])) * sl2;
+    return fmaxf(mt, S[15]);
+  };
+  // A masked key's weight 0 must not meet infinite or NaN values: they are
+  // cleared from this wave's share of a tile that may have masked keys, once it
+  // is there, and noted.
+  bool odd = false;
+  auto clear_odd = [&](int i, int buf) {
+    if (i < w.full_tiles || i >= t_last) return;
+#pragma unroll
+    for (int u = 0; u < CPW; ++u) {
+      uint4* at = (uint4*)&kv[ks][buf][1][((u * RS + rs) * 64 + lane) * 8];
+      const uint4 v = *at;
+      const uint4 z = make_uint4(finite_bf16(v.x), finite_bf16(v.y), finite_bf16(v.z), finite_bf16(v.w));
+      if (z.x != v.x || z.y != v.y || z.z != v.z || z.w != v.w) {
+        *at = z;
+        odd = true;
+      }
+    }
+  };
+  // softmax and V product of a tile whose lane maximum is mt; `between` goes
+  // next to the exponentials
+  auto finish = [&](f32x16& S, float mt, int buf, auto&& between) {
+    const uint16_t* vt = kv[ks][buf][1];
+    const float mp = pair_max(mt) * sl2;
     // the running maximum moves only when a tile exceeds it by 2^8
     const bool need = mp > m_run + 8.f;
     if (__ballot(need)) {
@@ -308,6 +336,7 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
 #pragma unroll
         for (int e = 0; e < 16; ++e) O[db][e] *= alpha;
     }
+    between();
     // the weights are rounded to bf16 for the V product; their sum, which lse
     // comes from, is taken before
     float p[16];
@@ -319,18 +348,6 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
     }
 #pragma unroll
     for (int e = 0; e < 16; e += 4) l_run += (p[e] + p[e + 1]) + (p[e + 2] + p[e + 3]);
-    // a masked key's infinite or NaN values must not meet its weight 0: in a
-    // tile that has such values they are left out of the product and added
-    // below for the rows that do see their key
-    bool odd = false;
-    if (masked) {
-      uint32_t any = 0;
-      for (int x = 0; x < TE / 512; ++x) {
-        const uint4 u = *(const uint4*)(vt + (x * 64 + lane) * 8);
-        any |= odd_bf16(u.x) | odd_bf16(u.y) | odd_bf16(u.z) | odd_bf16(u.w);
-      }
-      odd = __ballot(any != 0) != 0;
-    }
     const int grp = lane >> 4, gl = lane & 15;
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -341,58 +358,88 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
         const int key1 = key0 + 8;
         const v4i16 lo = lds_read_tr16(vt + (key0 * CH + ((dv >> 3) ^ kv_swz<D>(key0))) * 8 + (dv & 7));
         const v4i16 hi = lds_read_tr16(vt + (key1 * CH + ((dv >> 3) ^ kv_swz<D>(key1))) * 8 + (dv & 7));
-        auto v8 = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        if (odd) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if ((v8[e] & 0x7f80) == 0x7f80) v8[e] = 0;
-        }
-        O[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v8), P[x], O[db], 0, 0, 0);
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        O[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, P[x], O[db], 0, 0, 0);
       }
-    if (odd) {
-      for (int key = 0; key < kKeys; ++key) {
-        float pk = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (e == (key >> 3) * 4 + (key & 3)) pk = (float)P[e >> 3][e & 7];
-        pk = __shfl(pk, n + 32 * ((key >> 2) & 1));
-#pragma unroll
-        for (int db = 0; db < NDB; ++db)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int dv = db * 32 + (e >> 2) * 8 + h * 4 + (e & 3);
-            const uint16_t x = vt[(key * CH + ((dv >> 3) ^ kv_swz<D>(key))) * 8 + (dv & 7)];
-            if ((x & 0x7f80) == 0x7f80 && !(pk == 0.f)) O[db][e] += pk * bf16_bits_to_f32(x);
-          }
-      }
-    }
   };
 
-  if (RS == 1) {
+  if constexpr (RS == 1) {
     // a wave has its tiles to itself: no barriers, two tiles in flight
     int i = t_first + ks;
-    if (i < t_last) issue(i, 0);
-    if (i + KS < t_last) issue(i + KS, 1);
+    auto issue_tile = [&](int t, int buf) {
+      issue(t, 0, buf);
+      issue(t, 1, buf);
+    };
+    if (i < t_last) issue_tile(i, 0);
+    if (i + KS < t_last) issue_tile(i + KS, 1);
     for (int buf = 0; i < t_last; i += KS, buf ^= 1) {
       if (i + KS < t_last)
         wait_copies<2 * NCP>();
       else
         wait_copies<0>();
-      compute(i, buf);
+      f32x16 S;
+      scores(S, buf);
+      const float mt = mask_max(S, i);
+      clear_odd(i, buf);
+      finish(S, mt, buf, [] {});
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the buffer's reads are done
-      if (i + 2 * KS < t_last) issue(i + 2 * KS, buf);
+      if (i + 2 * KS < t_last) issue_tile(i + 2 * KS, buf);
     }
-  } else {
-    if (t_first + ks < t_last) issue(t_first + ks, 0);
-    int buf = 0;
-    for (int i0 = t_first; i0 < t_last; i0 += KS, buf ^= 1) {
+  } else if (t_first < t_last) {
+    // the waves of a tile share its copies; the scores of the next tile are
+    // formed next to the exponentials of this one, the copies of K run two
+    // tiles ahead and those of V one, with one barrier a step
+    const bool active = w.row0 + rs * 32 < w.rows;
+    int i = t_first + ks;  // this wave's tile
+    f32x16 S0, S1;
+    float mt = 0.f;
+    auto step = [&](int b, f32x16& Sc, f32x16& Sn) {
       wait_copies<0>();
-      __syncthreads();  // the step's tiles are there, the last step's have been read
-      if (i0 + KS + ks < t_last) issue(i0 + KS + ks, buf ^ 1);
-      if (i0 + ks < t_last) compute(i0 + ks, buf);
+      clear_odd(i, b);
+      __syncthreads();
+      if (i + 2 * KS < t_last) issue(i + 2 * KS, 0, b);
+      if (i + KS < t_last) issue(i + KS, 1, 1 - b);
+      if (active && i < t_last) {
+        finish(Sc, mt, b, [&] { scores(Sn, 1 - b); });
+        if (i + KS < t_last) mt = mask_max(Sn, i + KS);
+      }
+      i += KS;
+    };
+    if (i < t_last) issue(i, 0, 0), issue(i, 1, 0);
+    if (i + KS < t_last) issue(i + KS, 0, 1);
+    wait_copies<0>();
+    __syncthreads();
+    if (active && i < t_last) {
+      scores(S0, 0);
+      mt = mask_max(S0, i);
+    }
+    for (int i0 = t_first; i0 < t_last; i0 += 2 * KS) {
+      step(0, S0, S1);
+      if (i0 + KS < t_last) step(1, S1, S0);
     }
   }
   float l_tot = pair_sum(l_run);
+
+  // the values that were cleared, for the rows that see their keys: whatever
+  // the weight, they make a channel infinite or NaN
+  if (t_last > w.full_tiles && __syncthreads_or(odd)) {
+    for (int i = t_first + ks; i < t_last; i += KS) {
+      if (i < w.full_tiles) continue;
+      const uint32_t see = seen_keys(c, w, tree, i, valid, tok);
+      const bool old = i < w.old_tiles;
+      const int key0 = (old ? i : i - w.old_tiles) * kKeys, keys = min(kKeys, (old ? w.len : w.tok_end) - key0);
+      for (int key = 0; key < keys; ++key) {
+        const uint16_t* src = (const uint16_t*)(old ? vc : vn) + (int64_t)(key0 + key) * (old ? c.sn : c.nsn) + h * 4;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float x = bf16_bits_to_f32(src[db * 32 + (e >> 2) * 8 + (e & 3)]);
+            if (!__builtin_isfinite(x) && ((see >> key) & 1)) O[db][e] += x;
+          }
+      }
+    }
+  }
 
   // join the key tiles' waves of each set of rows
   if (KS > 1) {
@@ -528,6 +575,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(Cach
       for (int db = 0; db < NDB; ++db)
         O[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv[e][db], S[half * 8 + e], O[db], 0, 0, 0);
   };
+  bool odd = false;
   int i = w.t_first + ks;
   if (i < w.t_last) load_k(ka, i, 0);
   for (; i < w.t_last; i += KS) {
@@ -538,9 +586,9 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(Cach
     load_v(va, i, 0);
     scores(kb, 1);
     load_v(vb, i, 1);
-    bool masked;
-    const uint32_t see = seen_keys(c, w, tree, i, valid, tok, masked);
+    const bool masked = i >= w.full_tiles;
     if (masked) {
+      const uint32_t see = seen_keys(c, w, tree, i, valid, tok);
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (!((see >> ((e >> 2) * 8 + h * 4 + (e & 3))) & 1)) S[e] = -INFINITY;
@@ -565,42 +613,38 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(Cach
     for (int e = 0; e < 16; e += 4) l_run += (S[e] + S[e + 1]) + (S[e + 2] + S[e + 3]);
     // infinite and NaN values of masked keys, as in the bf16 kernel
     if (masked) {
-      bool any = false;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) any |= !__builtin_isfinite(va[e][db]) || !__builtin_isfinite(vb[e][db]);
-      if (__ballot(any)) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-          for (int db = 0; db < NDB; ++db) {
-            if (!__builtin_isfinite(va[e][db])) va[e][db] = 0.f;
-            if (!__builtin_isfinite(vb[e][db])) vb[e][db] = 0.f;
-          }
-        const bool old = i < w.old_tiles;
-        for (int key = 0; key < kKeys; ++key) {
-          float pk = 0.f;
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (e == (key >> 3) * 4 + (key & 3)) pk = S[e];
-          pk = __shfl(pk, n + 32 * ((key >> 2) & 1));
-          const float* src = (old ? vc : vn) + key_at(i, key) * (old ? c.sn : c.nsn);
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-#pragma unroll
-            for (int db = 0; db < NDB; ++db) {
-              const float x = src[((e >> 2) * 8 + 4 * h + (e & 3)) * NDB + db];
-              if (!__builtin_isfinite(x) && !(pk == 0.f)) O[db][e] += pk * x;
-            }
+        for (int db = 0; db < NDB; ++db) {
+          const bool fa = __builtin_isfinite(va[e][db]), fb = __builtin_isfinite(vb[e][db]);
+          odd |= !fa || !fb;
+          va[e][db] = fa ? va[e][db] : 0.f;
+          vb[e][db] = fb ? vb[e][db] : 0.f;
         }
-      }
     }
     pv(va, 0);
     if (i + KS < w.t_last) load_k(ka, i + KS, 0);
     pv(vb, 1);
   }
   float l_tot = pair_sum(l_run);
+  if (__ballot(odd)) {
+    for (i = w.t_first + ks; i < w.t_last; i += KS) {
+      if (i < w.full_tiles) continue;
+      const uint32_t see = seen_keys(c, w, tree, i, valid, tok);
+      const bool old = i < w.old_tiles;
+      for (int key = 0; key < kKeys; ++key) {
+        const float* src = (old ? vc : vn) + key_at(i, key) * (old ? c.sn : c.nsn);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) {
+            const float x = src[((e >> 2) * 8 + 4 * h + (e & 3)) * NDB + db];
+            if (!__builtin_isfinite(x) && ((see >> key) & 1)) O[db][e] += x;
+          }
+      }
+    }
+  }
   if (KS > 1) {
     if (ks > 0) {
       float(*dst)[64] = red[(ks - 1) * RS + rs];
@@ -643,17 +687,19 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(Cach
     c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok] = (m_run + log2f(l_tot)) * 0.6931471805599453f;
 }
 
-// Join the parts of the rows whose keys were split: one block a row, its
-// groups of D / 4 lanes taking the parts in turn.
-template <int D, int BF16>
+// Join the parts of the rows whose keys were split.  D / 4 lanes hold a row; a
+// block has 1,024 / D such groups, one a row (ALONE) or all on one row's parts
+// in turn: the latter where rows have many parts.
+template <int D, int BF16, bool ALONE>
 __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
   constexpr int L = D / 4, NG = 256 / L;
   __shared__ float4 so[NG][L];
   __shared__ float sl[NG];
   const int tid = threadIdx.x, lane = tid & 63, g = tid / L, i = tid % L;
-  const int R = c.T * c.G, row = blockIdx.x % R, bh = blockIdx.x / R, b = bh / c.Hkv, hk = bh % c.Hkv;
+  const int R = c.T * c.G, tiles = ALONE ? (R + NG - 1) / NG : R;
+  const int bh = blockIdx.x / tiles, row = ALONE ? blockIdx.x % tiles * NG + g : blockIdx.x % tiles;
+  const int b = bh / c.Hkv, hk = bh % c.Hkv;
   const int ntok = cache_count(c, b, c.T);
-  if (row >= ntok * c.G) return;
   const int per = part_steps(c, cut, lane);
   // this entry's parts follow those of the entries before it
   int first = 0;
@@ -662,16 +708,22 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
     first += wave_sum_i(st / per + (st % per != 0));
   }
   const int st = entry_steps(c, b, cut.ks), count = st / per + (st % per != 0);
-  if (count < 2) return;  // written by the part itself
+  // (one part wrote its rows itself)
+  if (count < 2 || row >= ntok * c.G || first + count > cut.slots) return;
   const size_t step = (size_t)c.Hkv * R;
   const size_t at = ((size_t)first * c.Hkv + hk) * R + row;
   float m = kNoMax;
-  for (int s = lane; s < count; s += 64) m = fmaxf(m, cut.ml[at + s * step].x);
-  m = wave_max(m);
+  if (ALONE) {
+#pragma unroll 4
+    for (int s = 0; s < count; ++s) m = fmaxf(m, cut.ml[at + s * step].x);
+  } else {
+    for (int s = lane; s < count; s += 64) m = fmaxf(m, cut.ml[at + s * step].x);
+    m = wave_max(m);
+  }
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int s = g; s < count; s += NG) {
+  for (int s = ALONE ? 0 : g; s < count; s += ALONE ? 1 : NG) {
     const float2 ml = cut.ml[at + s * step];
     const float4 x = *(const float4*)(cut.o + (at + s * step) * D + i * 4);
     const float f = __builtin_amdgcn_exp2f(ml.x - m);
@@ -681,17 +733,19 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
     o.z += x.z * f;
     o.w += x.w * f;
   }
-  so[g][i] = o;
-  if (i == 0) sl[g] = l;
-  __syncthreads();
-  if (g > 0) return;
-  for (int x = 1; x < NG; ++x) {
-    const float4 y = so[x][i];
-    o.x += y.x;
-    o.y += y.y;
-    o.z += y.z;
-    o.w += y.w;
-    l += sl[x];
+  if (!ALONE) {
+    so[g][i] = o;
+    if (i == 0) sl[g] = l;
+    __syncthreads();
+    if (g > 0) return;
+    for (int x = 1; x < NG; ++x) {
+      const float4 y = so[x][i];
+      o.x += y.x;
+      o.y += y.y;
+      o.z += y.z;
+      o.w += y.w;
+      l += sl[x];
+    }
   }
   const int tok = row / c.G, hq = hk * c.G + row % c.G;
   const int64_t dst = b * c.osb + hq * c.osh + tok * c.osn + i * 4;
@@ -731,7 +785,7 @@ size_t rows_of(const CacheCall& c, const Cut& cut) { return (size_t)cut.slots * 
 template <int D>
 void attend(const CacheCall& c, const Cut& cut, hipStream_t s) {
   const int64_t blocks = ((int64_t)cut.slots * c.Hkv * cut.row_tiles + 7) / 8 * 8;
-  const dim3 grid((unsigned)blocks), rows((unsigned)(c.B * c.Hkv * c.T * c.G));
+  const dim3 grid((unsigned)blocks);
   auto sets = [&](auto rs) {
     if (c.bf16)
       k_cache_attend<D, rs.value><<<grid, 256, 0, s>>>(c, cut);
@@ -744,10 +798,19 @@ void attend(const CacheCall& c, const Cut& cut, hipStream_t s) {
     default: sets(std::integral_constant<int, 4>{});
   }
   if (!cut.split) return;
-  if (c.bf16)
-    k_cache_join<D, 1><<<rows, 256, 0, s>>>(c, cut);
+  const int64_t heads = (int64_t)c.B * c.Hkv, R = (int64_t)c.T * c.G;
+  auto join = [&](auto alone) {
+    constexpr int NG = alone.value ? 1024 / D : 1;
+    const dim3 blocks((unsigned)(heads * ((R + NG - 1) / NG)));
+    if (c.bf16)
+      k_cache_join<D, 1, alone.value><<<blocks, 256, 0, s>>>(c, cut);
+    else
+      k_cache_join<D, 0, alone.value><<<blocks, 256, 0, s>>>(c, cut);
+  };
+  if (cut.parts <= 8)
+    join(std::true_type{});
   else
-    k_cache_join<D, 0><<<rows, 256, 0, s>>>(c, cut);
+    join(std::false_type{});
 }
 
 }  // namespace

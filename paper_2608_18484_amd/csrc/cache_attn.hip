@@ -37,7 +37,7 @@ struct Cut {
   int row_tiles;    // tiles of 32 RS rows of an entry and K/V head
   int ks;           // key tiles of a step
   int split;        // 0: one part per entry
-  int64_t parts;    // split: parts aimed at, over all entries (of each head and row tile)
+  int64_t parts;    // split: parts of all entries aimed at (of each head and row tile)
   int slots;        // parts of all entries at most
   float* o;         // [slots][Hkv][T G][D] parts' outputs, relative to their maxima
   float2* ml;       // [slots][Hkv][T G] maxima (base 2) and sums
@@ -761,11 +761,27 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
   if (i == 0 && c.lse) c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
+// Sets of 32 rows of a block.  One where that holds all rows: four waves then
+// stream four key tiles, which a step waits for alone.  Else four, or two where
+// an odd number of 64-row tiles would leave half a 128-row tile empty (189 rows
+// over two caches of 75,600 slots 178 us, with four sets 202; 576 rows 202 and
+// 213) and the rows are few: many rows read the keys from L2 once more for
+// every tile (4,680 rows over 18,720 keys 431 us, with two sets 492).
 int row_sets(const CacheCall& c) {
   const int64_t rows = (int64_t)c.T * c.G;
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  if (rows <= 32) return 1;
+  return rows <= 64 || ((rows + 63) / 64 % 2 == 1 && rows <= 640) ? 2 : 4;
 }
 
+// Parts.  A CU holds one block of the 128 KB of tiles of 32-row blocks at
+// d = 128 (or of fp32's registers) and two of the others; at d = 64 one such
+// block a CU streams as fast (45.9 us for two caches of 60,000 slots, with two
+// 47.6).  The parts of an entry end together when a launch fills the chip a
+// whole number of times, so that `parts`, of which ragged entries make up to
+// B - 1 more, is the most that r rounds hold; more rounds than one where a part
+// is then shorter by a twelfth (a frame's 296 blocks: one part each 566 us, 3
+// parts in two rounds 450, 5 in three 431; 24 blocks: 21 parts 178, 42 in two
+// rounds 187).
 Cut make_cut(const CacheCall& c) {
   Cut cut{};
   const int rs = row_sets(c);
@@ -773,10 +789,16 @@ Cut make_cut(const CacheCall& c) {
   cut.ks = 4 / rs;
   cut.row_tiles = (int)((rows + 32 * rs - 1) / (32 * rs));
   const int64_t units = (int64_t)c.Hkv * cut.row_tiles;  // blocks of a part
-  const int64_t aim = 1024;
-  cut.split = units * c.B < aim;
-  cut.parts = std::max<int64_t>(aim / units, 1);
-  cut.slots = c.B + (cut.split ? (int)cut.parts : 0);
+  const int64_t room = rs == 1 || (!c.bf16 && c.d == 128) ? 256 : 512;
+  double best = 1e30;
+  for (int r = 1; r <= 4; ++r) {
+    const int64_t parts = r * room / units - (c.B - 1);
+    if (parts <= c.B || r / (double)parts >= best * 0.92) continue;
+    best = r / (double)parts;
+    cut.parts = parts;
+  }
+  cut.split = cut.parts > 0;
+  cut.slots = c.B + (cut.split ? (int)cut.parts - 1 : 0);
   return cut;
 }
 

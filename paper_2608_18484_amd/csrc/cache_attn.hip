@@ -30,8 +30,6 @@ namespace sparsepr {
 
 namespace {
 
-constexpr int kKeys = 32;  // keys of a tile
-
 // How a launch is cut into blocks.
 struct Cut {
   int row_tiles;    // tiles of 32 RS rows of an entry and K/V head
@@ -49,54 +47,6 @@ __device__ __forceinline__ int entry_steps(const CacheCall& c, int b, int ks) {
   if (n == 0) return 0;
   const int tiles = (cache_length(c, b) + kKeys - 1) / kKeys + (n + kKeys - 1) / kKeys;
   return (tiles + ks - 1) / ks;
-}
-
-// Steps of a part: the same for all entries, so that blocks end together.
-__device__ __forceinline__ int part_steps(const CacheCall& c, const Cut& cut, int lane) {
-  if (!cut.split) return 0x7fffffff;
-  int64_t total = 0;
-  for (int b0 = 0; b0 < c.B; b0 += 64)
-    total += wave_sum_i(b0 + lane < c.B ? entry_steps(c, b0 + lane, cut.ks) : 0);
-  return (int)max((total + cut.parts - 1) / cut.parts, (int64_t)1);
-}
-
-// Entry and place of part `slot` among the parts of all entries, in the order
-// of the entries; `used` counts them all.  Called by whole waves.
-struct Part {
-  int b, first, last, count;  // entry, its steps [first, last), its parts
-};
-__device__ __forceinline__ int count_parts(const CacheCall& c, const Cut& cut, int per, int lane) {
-  int used = 0;
-  for (int b0 = 0; b0 < c.B; b0 += 64) {
-    const int st = b0 + lane < c.B ? entry_steps(c, b0 + lane, cut.ks) : 0;
-    used += wave_sum_i(st / per + (st % per != 0));
-  }
-  return used;
-}
-__device__ __forceinline__ Part find_part(const CacheCall& c, const Cut& cut, int per, int slot, int lane) {
-  Part p{-1, 0, 0, 0};
-  for (int b0 = 0; b0 < c.B; b0 += 64) {
-    const int st = b0 + lane < c.B ? entry_steps(c, b0 + lane, cut.ks) : 0;
-    const int n = st / per + (st % per != 0);
-    int upto = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(upto, o);
-      if (lane >= o) upto += y;
-    }
-    const uint64_t over = __ballot(upto > slot);
-    if (over) {
-      const int l = __builtin_ctzll(over);
-      const int at = slot - __shfl(upto - n, l), steps = __shfl(st, l);
-      p.b = b0 + l;
-      p.count = __shfl(n, l);
-      p.first = (int)min((int64_t)at * per, (int64_t)steps);
-      p.last = (int)min((int64_t)(at + 1) * per, (int64_t)steps);
-      return p;
-    }
-    slot -= __shfl(upto, 63);
-  }
-  return p;
 }
 
 // Every tree token's visible tokens as bits, by doubling: in round i a token
@@ -137,11 +87,6 @@ __device__ __forceinline__ void tree_bits(const CacheCall& c, int b, int n, Tree
   }
 }
 
-template <int N>
-__device__ __forceinline__ void wait_copies() {  // at most N of this wave's copies are under way
-  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
-}
-
 // Two bf16 values, 0 in the place of one that is infinite or NaN.
 __device__ __forceinline__ uint32_t finite_bf16(uint32_t x) {
   if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
@@ -162,15 +107,16 @@ struct Where {
 // use, the row tiles of a part and head next to each other, which read the
 // same keys.
 __device__ __forceinline__ bool locate(const CacheCall& c, const Cut& cut, int tile_rows, int lane, Where& w) {
-  const int per = part_steps(c, cut, lane);
-  const int64_t used = (int64_t)count_parts(c, cut, per, lane) * c.Hkv * cut.row_tiles;
+  auto steps = [&](int b) { return entry_steps(c, b, cut.ks); };
+  const int per = cut.split ? part_steps(c.B, cut.parts, lane, steps) : 0x7fffffff;
+  const int64_t used = (int64_t)count_parts(c.B, per, lane, steps) * c.Hkv * cut.row_tiles;
   const int64_t eighth = (used + 7) / 8;
   const int64_t at = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
   if ((int64_t)(blockIdx.x >> 3) >= eighth || at >= used) return false;
   const int rt = (int)(at % cut.row_tiles), unit = (int)(at / cut.row_tiles);
   w.hk = unit % c.Hkv;
   w.slot = unit / c.Hkv;
-  const Part part = find_part(c, cut, per, w.slot, lane);
+  const Part part = find_part(c.B, per, w.slot, lane, steps);
   if (part.b < 0 || w.slot >= cut.slots) return false;  // (only if lengths change during the launch)
   w.b = part.b;
   w.parts = part.count;
@@ -236,10 +182,6 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
   const char* vn = (const char*)((const uint16_t*)c.vn + b * c.nsb + hk * c.nsh);
   wait_copies<0>();
 
-  auto lds_of = [](const void* p) {
-    return __builtin_amdgcn_readfirstlane(
-        (uint32_t)(size_t)(const __attribute__((address_space(3))) void*)p);
-  };
   // copies of this wave's share of one of key tile i's tensors (0 = K, 1 = V);
   // rows past the end repeat the last one
   int ckey[CPW];
@@ -251,7 +193,7 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
     cchunk[u] = (uint32_t)(((s % CH) ^ kv_swz<D>(ckey[u])) * 16);
     voff[u] = (uint32_t)ckey[u] * (uint32_t)(c.sn * 2) + cchunk[u];
   }
-  const uint32_t kv_lds = lds_of(&kv[ks][0][0][0]) + rs * 1024;
+  const uint32_t kv_lds = lds_address(&kv[ks][0][0][0]) + rs * 1024;
   auto issue = [&](int i, int which, int buf) {
     const uint32_t dst = kv_lds + (uint32_t)(buf * 2 + which) * (TE * 2);
     if (i < w.full_tiles) {
@@ -700,14 +642,10 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
   const int bh = blockIdx.x / tiles, row = ALONE ? blockIdx.x % tiles * NG + g : blockIdx.x % tiles;
   const int b = bh / c.Hkv, hk = bh % c.Hkv;
   const int ntok = cache_count(c, b, c.T);
-  const int per = part_steps(c, cut, lane);
+  auto steps = [&](int e) { return entry_steps(c, e, cut.ks); };
+  const int per = part_steps(c.B, cut.parts, lane, steps);
   // this entry's parts follow those of the entries before it
-  int first = 0;
-  for (int b0 = 0; b0 < b; b0 += 64) {
-    const int st = b0 + lane < b ? entry_steps(c, b0 + lane, cut.ks) : 0;
-    first += wave_sum_i(st / per + (st % per != 0));
-  }
-  const int st = entry_steps(c, b, cut.ks), count = st / per + (st % per != 0);
+  const int first = count_parts(b, per, lane, steps), count = parts_of(steps(b), per);
   // (one part wrote its rows itself)
   if (count < 2 || row >= ntok * c.G || first + count > cut.slots) return;
   const size_t step = (size_t)c.Hkv * R;

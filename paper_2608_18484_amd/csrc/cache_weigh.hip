@@ -26,6 +26,7 @@ struct WeighCut {
   int key_blocks;  // blocks of keys of an entry and K/V head at most
   int parts_max;   // row parts at most; 1: sums go straight to the scores
   int aim;         // blocks aimed at
+  int64_t parts;   // few rows: parts of all entries aimed at (of each head)
   float* sums;     // [parts_max][B Hkv][cap]
 };
 
@@ -187,6 +188,127 @@ __global__ __launch_bounds__(256, 2) void k_cache_accumulate(CacheCall c, WeighC
   }
 }
 
+// At most 32 rows: their operands stay in registers and the keys stream by.
+// Every wave walks key tiles of its own through LDS, NB of them on the way by
+// direct copies, so that the launch runs at the rate at which K arrives; the
+// slots' scores come along with the keys (a load of their own would wait for
+// the copies behind it).
+template <int D, class E>
+__global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w) {
+  constexpr int EPC = 16 / sizeof(E);
+  constexpr int CH = D / EPC, NF = CH / 2;
+  constexpr int NCP = kKeys * CH / 64;         // 1 KB copies of a tile
+  constexpr int NB = NCP <= 4 ? 4 : NCP <= 8 ? 4 : 2;
+  constexpr int SW = CH == 8 ? 64 : 128;
+  __shared__ __attribute__((aligned(1024))) uint4 kt[4][NB][kKeys * CH];
+  __shared__ float st[4][NB][64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, h = lane >> 5;
+  auto steps = [&](int b) { return (cache_length(c, b) + 4 * kKeys - 1) / (4 * kKeys); };
+  const int per = part_steps(c.B, w.parts, lane, steps);
+  const int slot = blockIdx.x / c.Hkv, hk = blockIdx.x % c.Hkv;
+  const Part part = find_part(c.B, per, slot, lane, steps);
+  if (part.b < 0) return;
+  const int b = part.b, len = cache_length(c, b), ntok = cache_count(c, b, c.C);
+  const int rows = ntok * c.G;
+  if (rows == 0) return;
+  // this lane's row of the operand; the rows of its score registers
+  auto row_of = [&](int r, int& tok) {  // what row r sees
+    const int i = r / c.G;
+    tok = 0;
+    if (r >= rows) return 0;
+    tok = c.rows ? c.rows[(size_t)b * c.C + i] : i;
+    if (tok < 0 || tok >= c.T) {
+      if (part.first == 0 && hk == 0) raise_flag(c, b, SPARSEPR_CACHE_FLAG_BAD_INDEX);
+      tok = 0;
+      return 0;
+    }
+    return c.mask == SPARSEPR_TOKENS_FULL ? len : min(max(len - ntok + i + 1, 0), len);
+  };
+  int tok;
+  int sees = row_of(n, tok);
+  const int hq = hk * c.G + n % c.G;
+  uint4 q[NF];
+  {
+    const E* src = (const E*)c.q + b * c.qsb + hq * c.qsh + tok * c.qsn + h * EPC;
+#pragma unroll
+    for (int x = 0; x < NF; ++x) q[x] = *(const uint4*)(src + x * 2 * EPC);
+  }
+  float z = c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok];
+  if (z == -INFINITY) sees = 0;
+  if (sees == 0) z = 0.f;
+  float zr[16];
+  int vr[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int r = (e >> 2) * 8 + h * 4 + (e & 3);
+    zr[e] = __shfl(z, r) * 1.4426950408889634f;
+    vr[e] = __shfl(sees, r);
+  }
+  const char* kc = (const char*)((const E*)c.k + b * c.sb + hk * c.sh);
+  float* score = c.scores + ((size_t)b * c.Hkv + hk) * c.cap;
+  const int tiles = (len + kKeys - 1) / kKeys, full_tiles = len / kKeys;
+  const int t_last = min(part.last * 4, tiles);
+  const uint32_t stride = (uint32_t)(c.sn * sizeof(E));
+  int ckey[NCP];
+  uint32_t cchunk[NCP];
+#pragma unroll
+  for (int u = 0; u < NCP; ++u) {
+    const int s = u * 64 + lane;
+    ckey[u] = s / CH;
+    cchunk[u] = (uint32_t)(((s % CH) ^ kv_swz<SW>(ckey[u])) * 16);
+  }
+  const uint32_t k_lds = lds_address(&kt[wv][0][0]), s_lds = lds_address(&st[wv][0][0]);
+  auto issue = [&](int i, int buf) {
+    const char* p = kc + (int64_t)i * kKeys * stride;
+    const int left = i < full_tiles ? kKeys - 1 : len - i * kKeys - 1;  // rows past the end repeat the last one
+#pragma unroll
+    for (int u = 0; u < NCP; ++u)
+      g2lds16s(p, (uint32_t)min(ckey[u], left) * stride + cchunk[u], k_lds + buf * (kKeys * CH * 16) + u * 1024);
+    g2lds4s(score + i * kKeys, (uint32_t)min(n, left) * 4, s_lds + buf * 256);
+  };
+  wait_copies<0>();
+  const float sl2 = 1.4426950408889634f / sqrtf((float)D);
+  int i = part.first * 4 + wv;
+  // a wave always has NB tiles under way; those past its last repeat it
+  const int i_last = i < t_last ? i + (t_last - 1 - i) / 4 * 4 : i;
+  if (i >= t_last) return;
+#pragma unroll
+  for (int x = 0; x < NB; ++x) issue(min(i + x * 4, i_last), x);
+  for (int buf = 0; i < t_last; i += 4, buf = buf + 1 == NB ? 0 : buf + 1) {
+    wait_copies<(NB - 1) * (NCP + 1)>();
+    const uint4* k = kt[wv][buf];
+    f32x16 S;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) S[e] = 0.f;
+#pragma unroll
+    for (int x = 0; x < NF; ++x) {
+      const uint4 kf = k[n * CH + ((2 * x + h) ^ kv_swz<SW>(n))];
+      if constexpr (sizeof(E) == 2) {
+        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, q[x]), __builtin_bit_cast(bf16x8, kf), S, 0, 0, 0);
+      } else {
+        const f32x4 qa = __builtin_bit_cast(f32x4, q[x]), ka = __builtin_bit_cast(f32x4, kf);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_32x32x2f32(qa[e], ka[e], S, 0, 0, 0);
+      }
+    }
+    const int j = i * kKeys + n;
+    const float old = st[wv][buf][lane];
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(S[e], sl2, -zr[e]));
+      sum += j < vr[e] ? p : 0.f;
+    }
+    sum = pair_sum(sum);
+    if (h == 0 && j < len) score[j] = old + sum;
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the buffer's reads are done
+    issue(min(i + NB * 4, i_last), buf);
+  }
+  wait_copies<0>();
+}
+
 // The row parts' sums, in their order, into the scores.
 __global__ __launch_bounds__(256) void k_cache_weigh_join(CacheCall c, WeighCut w, int keys) {
   const int bh = blockIdx.y, len = cache_length(c, bh / c.Hkv), j = blockIdx.x * 256 + threadIdx.x;
@@ -197,6 +319,8 @@ __global__ __launch_bounds__(256) void k_cache_weigh_join(CacheCall c, WeighCut 
   for (int p = 0; p < parts; ++p) v += w.sums[p * step + o];
   c.scores[o] += v;
 }
+
+constexpr int kRoom = 256;  // blocks of k_cache_weigh_few aimed at
 
 constexpr int weigh_keys(bool bf16) { return bf16 ? 256 : 128; }
 
@@ -210,15 +334,27 @@ WeighCut weigh_cut(const CacheCall& c) {
   return w;
 }
 
+bool few_rows(const CacheCall& c) { return (int64_t)c.C * c.G <= 32; }
+
 }  // namespace
 
 size_t cache_accumulate_workspace(const CacheCall& c) {
+  if (few_rows(c)) return 0;
   const WeighCut w = weigh_cut(c);
   return w.parts_max == 1 ? 0 : (size_t)w.parts_max * c.B * c.Hkv * c.cap * 4;
 }
 
 void launch_cache_accumulate(const CacheCall& c, void* ws, hipStream_t s) {
   WeighCut w = weigh_cut(c);
+  if (few_rows(c)) {
+    w.parts = std::max<int64_t>(kRoom / c.Hkv - (c.B - 1), c.B);
+    const dim3 grid((unsigned)((w.parts + c.B - 1) * c.Hkv));
+    if (c.bf16)
+      c.d == 64 ? k_cache_weigh_few<64, uint16_t><<<grid, 256, 0, s>>>(c, w) : k_cache_weigh_few<128, uint16_t><<<grid, 256, 0, s>>>(c, w);
+    else
+      c.d == 64 ? k_cache_weigh_few<64, float><<<grid, 256, 0, s>>>(c, w) : k_cache_weigh_few<128, float><<<grid, 256, 0, s>>>(c, w);
+    return;
+  }
   w.sums = (float*)ws;
   const int64_t blocks = ((int64_t)c.B * c.Hkv * w.parts_max * w.key_blocks + 7) / 8 * 8;
   const dim3 grid((unsigned)blocks);

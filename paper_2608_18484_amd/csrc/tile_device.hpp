@@ -64,6 +64,19 @@ __device__ __forceinline__ void g2lds16s(const void* sbase, uint32_t voff, uint3
                : "memory");
 }
 
+// The same for 4 bytes per lane, at m0v + 4*l.
+__device__ __forceinline__ void g2lds4s(const void* sbase, uint32_t voff, uint32_t m0v) {
+  const uint64_t b = (uint64_t)(size_t)sbase;
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
+  const uint64_t sb = ((uint64_t)hi << 32) | (uint64_t)lo;
+  const uint32_t m0u = (uint32_t)__builtin_amdgcn_readfirstlane(m0v);
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1 offset:0"
+               :
+               : "v"(voff), "s"(sb), "s"(m0u)
+               : "memory");
+}
+
 // Combine a value with the one held by lane l ^ 32 (the other half of the
 // same query's keys) through v_permlane32_swap: swapping a register with
 // itself leaves, in each lane, its own value in one result and its partner's

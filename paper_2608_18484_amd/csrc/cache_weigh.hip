@@ -25,36 +25,101 @@ namespace {
 struct WeighCut {
   int key_blocks;  // blocks of keys of an entry and K/V head at most
   int parts_max;   // row parts at most; 1: sums go straight to the scores
-  int aim;         // blocks aimed at
+  int tiles_max;   // row tiles of an entry and K/V head at most
   int64_t parts;   // few rows: parts of all entries aimed at (of each head)
+  char* rows;      // [B Hkv][tiles_max] row tiles as they go to LDS
+  float* zv;       // [B Hkv][tiles_max][2][32] the rows' lse (base 2), and the slots they see
+  int2* span;      // [B Hkv][tiles_max] the fewest and the most slots that a row of the tile sees
   float* sums;     // [parts_max][B Hkv][cap]
 };
 
-// Row parts: as many as bring the blocks in use to the number aimed at.
+constexpr int kWeighRoom = 512;  // blocks of k_cache_accumulate that the chip holds
+
+// Row parts: the number whose blocks fill the chip a whole number of times best.
 __device__ __forceinline__ int weigh_parts(const CacheCall& c, const WeighCut& w, int keys, int lane) {
   if (w.parts_max == 1) return 1;
   int used = 0;
   for (int b0 = 0; b0 < c.B; b0 += 64)
     used += wave_sum_i(b0 + lane < c.B ? (cache_length(c, b0 + lane) + keys - 1) / keys : 0);
-  return min(w.parts_max, max(1, w.aim / max(1, used * c.Hkv)));
+  used *= c.Hkv;
+  int best = 1;
+  for (int p = 2; p <= w.parts_max; ++p) {
+    const int64_t now = (used * (int64_t)p + kWeighRoom - 1) / kWeighRoom, was = (used * (int64_t)best + kWeighRoom - 1) / kWeighRoom;
+    if (now * best * 16 < was * p * 15) best = p;
+  }
+  return best;
+}
+
+// Which chunk of 16 bytes of a row of CH sits at place x of the row in LDS, and
+// the other way round.
+template <int CH>
+__device__ __forceinline__ int row_swz(int r) {
+  return kv_swz<CH == 8 ? 64 : 128>(r);
+}
+
+// A row of the list: token i, query head g.  What it sees, its token.
+__device__ __forceinline__ int row_sees(const CacheCall& c, int b, int len, int ntok, int i, bool flag, int& tok) {
+  tok = 0;
+  if (i >= ntok) return 0;
+  const int x = c.rows ? c.rows[(size_t)b * c.C + i] : i;
+  if (x < 0 || x >= c.T) {
+    if (flag) raise_flag(c, b, SPARSEPR_CACHE_FLAG_BAD_INDEX);
+    return 0;
+  }
+  tok = x;
+  return c.mask == SPARSEPR_TOKENS_FULL ? len : min(max(len - ntok + i + 1, 0), len);
+}
+
+// The rows gathered once into tiles of 32, laid out as every block that they
+// pass by copies them to LDS.
+template <int D, class E>
+__global__ __launch_bounds__(256) void k_cache_weigh_rows(CacheCall c, WeighCut w) {
+  constexpr int EPC = 16 / sizeof(E), CH = D / EPC;
+  const int t = blockIdx.x % w.tiles_max, bh = blockIdx.x / w.tiles_max, b = bh / c.Hkv, hk = bh % c.Hkv;
+  const int len = cache_length(c, b), ntok = cache_count(c, b, c.C), tid = threadIdx.x;
+  if (t * 32 >= ntok * c.G) return;
+  const size_t at = (size_t)bh * w.tiles_max + t;
+  uint4* dst = (uint4*)w.rows + at * 32 * CH;
+#pragma unroll
+  for (int u = 0; u < 32 * CH / 256; ++u) {
+    const int s = u * 256 + tid, r = s / CH, row = t * 32 + r;
+    int tok;
+    (void)row_sees(c, b, len, ntok, row / c.G, false, tok);
+    dst[r * CH + ((s % CH) ^ row_swz<CH>(r))] =
+        *(const uint4*)((const E*)c.q + b * c.qsb + (hk * c.G + row % c.G) * c.qsh + tok * c.qsn + (s % CH) * EPC);
+  }
+  if (tid >= 64) return;
+  const int row = t * 32 + (tid & 31), hq = hk * c.G + row % c.G;
+  int tok;
+  int vis = row_sees(c, b, len, ntok, row / c.G, hk == 0 && tid < 32, tok);
+  float z = c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok];
+  if (z == -INFINITY) vis = 0;
+  if (vis == 0) z = 0.f;
+  w.zv[at * 64 + tid] = tid < 32 ? z * 1.4426950408889634f : __int_as_float(vis);
+  int lo = vis, hi = vis;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    lo = min(lo, __shfl_xor(lo, o));
+    hi = max(hi, __shfl_xor(hi, o));
+  }
+  if (tid == 0) w.span[at] = make_int2(lo, hi);
 }
 
 // E: element type; SETS: sets of 32 keys of a wave.
 template <int D, class E, int SETS>
 __global__ __launch_bounds__(256, 2) void k_cache_accumulate(CacheCall c, WeighCut w) {
-  constexpr int EPC = 16 / sizeof(E);      // elements of a 16-byte chunk
+  constexpr int EPC = 16 / sizeof(E);       // elements of a 16-byte chunk
   constexpr int CH = D / EPC, NF = CH / 2;  // chunks of a row; operands of a lane
   constexpr int KEYS = 128 * SETS;          // keys of a block
-  constexpr int LD = 32 * CH / 256;         // chunks of a row tile that a thread loads
-  __shared__ uint4 qt[2][32 * CH];
-  __shared__ float zt[2][32];
-  __shared__ int vt[2][32];
-  __shared__ int masked[2];
+  constexpr int NCP = 32 * CH / 64;         // 1 KB copies of a tile of rows
+  constexpr int CPW = NCP / 4;              // of a wave
+  constexpr int NB = 3;
+  __shared__ __attribute__((aligned(1024))) uint4 mem[KEYS * CH];  // keys at first, then NB tiles of rows
+  __shared__ float zv[NB][64];
+  static_assert(NB * 32 <= KEYS, "rows fit the keys' memory");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
-  constexpr int SW = CH == 8 ? 64 : 128;  // the swizzle of 128-byte rows or of longer ones
-  auto swz = [](int r) { return kv_swz<SW>(r); };
 
   // XCD x takes the x-th eighth of the blocks: its L2 holds few heads' rows
   const int parts = weigh_parts(c, w, KEYS, lane);
@@ -68,73 +133,62 @@ __global__ __launch_bounds__(256, 2) void k_cache_accumulate(CacheCall c, WeighC
   const int tiles = (ntok * c.G + 31) / 32;
   const int t_first = (int)((int64_t)tiles * part / parts), t_last = (int)((int64_t)tiles * (part + 1) / parts);
 
-  // this wave's keys (past the end: the last one, not stored)
+  // this wave's keys through its share of the memory (past the end: the last
+  // one, not stored)
   const int key0 = kb * KEYS + wv * 32 * SETS;
   uint4 kf[SETS][NF];
+  {
+    const char* src = (const char*)((const E*)c.k + b * c.sb + hk * c.sh) + (int64_t)key0 * (int64_t)(c.sn * sizeof(E));
+    const int left = max(len - 1 - key0, 0);
+    const char* base = key0 < len ? src : (const char*)((const E*)c.k + b * c.sb + hk * c.sh);
+    const uint32_t lds = lds_address(mem) + (uint32_t)(wv * 32 * SETS * CH * 16);
 #pragma unroll
-  for (int s = 0; s < SETS; ++s) {
-    const E* src = (const E*)c.k + b * c.sb + hk * c.sh + (int64_t)min(key0 + s * 32 + n, len - 1) * c.sn + h * EPC;
+    for (int u = 0; u < NCP * SETS; ++u) {
+      const int s = u * 64 + lane, r = s / CH;
+      g2lds16s(base, (uint32_t)min(r, left) * (uint32_t)(c.sn * sizeof(E)) + (uint32_t)(((s % CH) ^ row_swz<CH>(r & 31)) * 16), lds + u * 1024);
+    }
+    wait_copies<0>();
+    const uint4* kt = mem + wv * 32 * SETS * CH;
 #pragma unroll
-    for (int x = 0; x < NF; ++x) kf[s][x] = *(const uint4*)(src + x * 2 * EPC);
+    for (int s = 0; s < SETS; ++s)
+#pragma unroll
+      for (int x = 0; x < NF; ++x) kf[s][x] = kt[(s * 32 + n) * CH + ((2 * x + h) ^ row_swz<CH>(n))];
   }
   float sum[SETS];
 #pragma unroll
   for (int s = 0; s < SETS; ++s) sum[s] = 0.f;
 
-  // rows of tile t: token i of the list, query head g
-  const int full = c.mask == SPARSEPR_TOKENS_FULL;
-  auto sees = [&](int i) { return i >= ntok ? 0 : full ? len : min(max(len - ntok + i + 1, 0), len); };
-  uint4 qr[LD];
-  float z = 0.f;
-  int vis = 0;
-  auto token = [&](int i) { return c.rows ? c.rows[(size_t)b * c.C + i] : i; };
-  auto fetch = [&](int t) {
+  const size_t tile0 = (size_t)bh * w.tiles_max;
+  const uint32_t q_lds = lds_address(mem), z_lds = lds_address(zv);
+  const int last = max(t_last - 1, 0);
+  // copies of a tile of rows, each wave's share (tiles past the last repeat it)
+  auto issue = [&](int t, int buf) {
+    t = min(t, last);
+    const char* src = w.rows + (tile0 + t) * (32 * CH * 16);
 #pragma unroll
-    for (int u = 0; u < LD; ++u) {
-      const int s = u * 256 + tid, r = min(t * 32 + s / CH, ntok * c.G - 1);
-      const int tok = min(max(token(r / c.G), 0), c.T - 1);
-      qr[u] = *(const uint4*)((const E*)c.q + b * c.qsb + (hk * c.G + r % c.G) * c.qsh + tok * c.qsn + (s % CH) * EPC);
-    }
-    if (tid < 32) {
-      const int r = t * 32 + tid, i = r / c.G;
-      vis = sees(i);
-      z = 0.f;
-      if (i < ntok) {
-        const int tok = token(i);
-        const bool bad = tok < 0 || tok >= c.T;
-        if (bad && kb == 0) raise_flag(c, b, SPARSEPR_CACHE_FLAG_BAD_INDEX);
-        if (!bad) z = c.lse[((size_t)b * c.Hkv * c.G + hk * c.G + r % c.G) * c.T + tok];
-        if (bad || z == -INFINITY) vis = 0, z = 0.f;
-      }
-    }
+    for (int u = 0; u < CPW; ++u)
+      g2lds16s(src, (uint32_t)((u * 4 + wv) * 1024 + lane * 16), q_lds + buf * (32 * CH * 16) + (u * 4 + wv) * 1024);
+    if (wv == 0) g2lds4s(w.zv + (tile0 + t) * 64, (uint32_t)lane * 4, z_lds + buf * 256);
   };
-  auto store = [&](int t, int buf) {
-#pragma unroll
-    for (int u = 0; u < LD; ++u) {
-      const int s = u * 256 + tid, r = s / CH;
-      qt[buf][r * CH + ((s % CH) ^ swz(r))] = qr[u];
-    }
-    if (tid < 64) {
-      // rows that see less than their place says (or are none)
-      const bool odd = tid < 32 && vis != sees((t * 32 + tid) / c.G);
-      const uint64_t any = __ballot(odd);
-      if (tid < 32) {
-        zt[buf][tid] = z * 1.4426950408889634f;
-        vt[buf][tid] = vis;
-      }
-      if (tid == 0) masked[buf] = any != 0 || (t * 32 + 31) / c.G >= ntok;
-    }
-  };
+  asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+  __builtin_amdgcn_s_barrier();  // every wave has its keys
   const float sl2 = 1.4426950408889634f / sqrtf((float)D);
-  if (t_first < t_last) fetch(t_first);
+  if (t_first < t_last) {
+    issue(t_first, 0);
+    issue(t_first + 1, 1);
+  }
   int buf = 0;
-  for (int t = t_first; t < t_last; ++t, buf ^= 1) {
-    store(t, buf);
-    __syncthreads();
-    if (t + 1 < t_last) fetch(t + 1);
-    // what the tile's first and last row see at least and at most
-    const int lo = masked[buf] ? 0 : sees(t * 32 / c.G), hi = sees(min((t * 32 + 31) / c.G, ntok - 1));
-    if (key0 >= hi) continue;
+  for (int t = t_first; t < t_last; ++t) {
+    const int2 span = w.span[tile0 + t];
+    wait_copies<CPW>();  // this tile's copies are there, the next one's may be under way
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    const int ahead = buf == 0 ? 2 : buf - 1;  // the buffer of the last tile
+    issue(t + 2, ahead);
+    const uint4* qt = mem + buf * 32 * CH;
+    const float* zt = zv[buf];
+    buf = buf == 2 ? 0 : buf + 1;
+    if (key0 >= span.y) continue;
     f32x16 S[SETS];
 #pragma unroll
     for (int s = 0; s < SETS; ++s)
@@ -142,7 +196,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_accumulate(CacheCall c, WeighC
       for (int e = 0; e < 16; ++e) S[s][e] = 0.f;
 #pragma unroll
     for (int x = 0; x < NF; ++x) {
-      const uint4 q = qt[buf][n * CH + ((2 * x + h) ^ swz(n))];
+      const uint4 q = qt[n * CH + ((2 * x + h) ^ row_swz<CH>(n))];
 #pragma unroll
       for (int s = 0; s < SETS; ++s) {
         if constexpr (sizeof(E) == 2) {
@@ -155,25 +209,34 @@ __global__ __launch_bounds__(256, 2) void k_cache_accumulate(CacheCall c, WeighC
       }
     }
     // register e: row (e / 4) 8 + h 4 + e % 4
+    const bool masked = key0 + SETS * 32 > span.x;
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
-      const float4 zz = *(const float4*)&zt[buf][e4 * 8 + h * 4];
+      const float4 zz = *(const float4*)(zt + e4 * 8 + h * 4);
       const float zr[4] = {zz.x, zz.y, zz.z, zz.w};
 #pragma unroll
-      for (int s = 0; s < SETS; ++s) {
-        float p[4];
+      for (int s = 0; s < SETS; ++s)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(S[s][e4 * 4 + e], sl2, -zr[e]));
-        if (key0 + s * 32 + 31 >= lo) {
-          const int4 vv = *(const int4*)&vt[buf][e4 * 8 + h * 4];
-          const int vr[4] = {vv.x, vv.y, vv.z, vv.w}, j = key0 + s * 32 + n;
+        for (int e = 0; e < 4; ++e) S[s][e4 * 4 + e] = __builtin_amdgcn_exp2f(fmaf(S[s][e4 * 4 + e], sl2, -zr[e]));
+    }
+    if (masked) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = j < vr[e] ? p[e] : 0.f;
-        }
-        sum[s] += (p[0] + p[1]) + (p[2] + p[3]);
+      for (int e4 = 0; e4 < 4; ++e4) {
+        const int4 vv = *(const int4*)(zt + 32 + e4 * 8 + h * 4);
+        const int vr[4] = {vv.x, vv.y, vv.z, vv.w};
+#pragma unroll
+        for (int s = 0; s < SETS; ++s)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (key0 + s * 32 + n >= vr[e]) S[s][e4 * 4 + e] = 0.f;
       }
     }
+#pragma unroll
+    for (int s = 0; s < SETS; ++s)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) sum[s] += (S[s][e] + S[s][e + 1]) + (S[s][e + 2] + S[s][e + 3]);
   }
+  wait_copies<0>();
 #pragma unroll
   for (int s = 0; s < SETS; ++s) {
     const float v = pair_sum(sum[s]);
@@ -199,7 +262,6 @@ __global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w
   constexpr int CH = D / EPC, NF = CH / 2;
   constexpr int NCP = kKeys * CH / 64;         // 1 KB copies of a tile
   constexpr int NB = NCP <= 4 ? 4 : NCP <= 8 ? 4 : 2;
-  constexpr int SW = CH == 8 ? 64 : 128;
   __shared__ __attribute__((aligned(1024))) uint4 kt[4][NB][kKeys * CH];
   __shared__ float st[4][NB][64];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -214,20 +276,8 @@ __global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w
   const int rows = ntok * c.G;
   if (rows == 0) return;
   // this lane's row of the operand; the rows of its score registers
-  auto row_of = [&](int r, int& tok) {  // what row r sees
-    const int i = r / c.G;
-    tok = 0;
-    if (r >= rows) return 0;
-    tok = c.rows ? c.rows[(size_t)b * c.C + i] : i;
-    if (tok < 0 || tok >= c.T) {
-      if (part.first == 0 && hk == 0) raise_flag(c, b, SPARSEPR_CACHE_FLAG_BAD_INDEX);
-      tok = 0;
-      return 0;
-    }
-    return c.mask == SPARSEPR_TOKENS_FULL ? len : min(max(len - ntok + i + 1, 0), len);
-  };
   int tok;
-  int sees = row_of(n, tok);
+  int sees = row_sees(c, b, len, ntok, n / c.G, part.first == 0 && hk == 0, tok);
   const int hq = hk * c.G + n % c.G;
   uint4 q[NF];
   {
@@ -257,7 +307,7 @@ __global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w
   for (int u = 0; u < NCP; ++u) {
     const int s = u * 64 + lane;
     ckey[u] = s / CH;
-    cchunk[u] = (uint32_t)(((s % CH) ^ kv_swz<SW>(ckey[u])) * 16);
+    cchunk[u] = (uint32_t)(((s % CH) ^ row_swz<CH>(ckey[u])) * 16);
   }
   const uint32_t k_lds = lds_address(&kt[wv][0][0]), s_lds = lds_address(&st[wv][0][0]);
   auto issue = [&](int i, int buf) {
@@ -284,7 +334,7 @@ __global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w
     for (int e = 0; e < 16; ++e) S[e] = 0.f;
 #pragma unroll
     for (int x = 0; x < NF; ++x) {
-      const uint4 kf = k[n * CH + ((2 * x + h) ^ kv_swz<SW>(n))];
+      const uint4 kf = k[n * CH + ((2 * x + h) ^ row_swz<CH>(n))];
       if constexpr (sizeof(E) == 2) {
         S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, q[x]), __builtin_bit_cast(bf16x8, kf), S, 0, 0, 0);
       } else {
@@ -329,19 +379,38 @@ WeighCut weigh_cut(const CacheCall& c) {
   const int keys = weigh_keys(c.bf16);
   WeighCut w{};
   w.key_blocks = (c.cap + keys - 1) / keys;
-  w.aim = 2048;
+  w.tiles_max = (int)tiles;
   w.parts_max = (int)std::max<int64_t>(1, std::min<int64_t>(8, tiles / 8));
   return w;
 }
 
 bool few_rows(const CacheCall& c) { return (int64_t)c.C * c.G <= 32; }
 
+// Bytes of the workspace's arrays, in their order.
+size_t weigh_bytes(const CacheCall& c, const WeighCut& w, size_t* rows, size_t* zv, size_t* span) {
+  const size_t tiles = (size_t)c.B * c.Hkv * w.tiles_max;
+  *rows = tiles * 32 * c.d * (c.bf16 ? 2 : 4);
+  *zv = tiles * 256;
+  *span = tiles * 8;
+  const size_t sums = w.parts_max == 1 ? 0 : (size_t)w.parts_max * c.B * c.Hkv * c.cap * 4;
+  return *rows + *zv + *span + sums;
+}
+
+template <int D, class E, int SETS>
+void weigh(const CacheCall& c, const WeighCut& w, hipStream_t s) {
+  const int64_t heads = (int64_t)c.B * c.Hkv;
+  k_cache_weigh_rows<D, E><<<(unsigned)(heads * w.tiles_max), 256, 0, s>>>(c, w);
+  const int64_t blocks = (heads * w.parts_max * w.key_blocks + 7) / 8 * 8;
+  k_cache_accumulate<D, E, SETS><<<(unsigned)blocks, 256, 0, s>>>(c, w);
+  if (w.parts_max > 1)
+    k_cache_weigh_join<<<dim3((c.cap + 255) / 256, (unsigned)heads), 256, 0, s>>>(c, w, 128 * SETS);
+}
+
 }  // namespace
 
 size_t cache_accumulate_workspace(const CacheCall& c) {
-  if (few_rows(c)) return 0;
-  const WeighCut w = weigh_cut(c);
-  return w.parts_max == 1 ? 0 : (size_t)w.parts_max * c.B * c.Hkv * c.cap * 4;
+  size_t rows, zv, span;
+  return few_rows(c) ? 0 : weigh_bytes(c, weigh_cut(c), &rows, &zv, &span);
 }
 
 void launch_cache_accumulate(const CacheCall& c, void* ws, hipStream_t s) {
@@ -355,17 +424,16 @@ void launch_cache_accumulate(const CacheCall& c, void* ws, hipStream_t s) {
       c.d == 64 ? k_cache_weigh_few<64, float><<<grid, 256, 0, s>>>(c, w) : k_cache_weigh_few<128, float><<<grid, 256, 0, s>>>(c, w);
     return;
   }
-  w.sums = (float*)ws;
-  const int64_t blocks = ((int64_t)c.B * c.Hkv * w.parts_max * w.key_blocks + 7) / 8 * 8;
-  const dim3 grid((unsigned)blocks);
+  size_t rows, zv, span;
+  (void)weigh_bytes(c, w, &rows, &zv, &span);
+  w.rows = (char*)ws;
+  w.zv = (float*)(w.rows + rows);
+  w.span = (int2*)((char*)w.zv + zv);
+  w.sums = (float*)((char*)w.span + span);
   if (c.bf16)
-    c.d == 64 ? k_cache_accumulate<64, uint16_t, 2><<<grid, 256, 0, s>>>(c, w)
-              : k_cache_accumulate<128, uint16_t, 2><<<grid, 256, 0, s>>>(c, w);
+    c.d == 64 ? weigh<64, uint16_t, 2>(c, w, s) : weigh<128, uint16_t, 2>(c, w, s);
   else
-    c.d == 64 ? k_cache_accumulate<64, float, 1><<<grid, 256, 0, s>>>(c, w)
-              : k_cache_accumulate<128, float, 1><<<grid, 256, 0, s>>>(c, w);
-  if (w.parts_max > 1)
-    k_cache_weigh_join<<<dim3((c.cap + 255) / 256, c.B * c.Hkv), 256, 0, s>>>(c, w, weigh_keys(c.bf16));
+    c.d == 64 ? weigh<64, float, 1>(c, w, s) : weigh<128, float, 1>(c, w, s);
 }
 
 }  // namespace sparsepr

@@ -25,6 +25,7 @@ namespace {
 struct WeighCut {
   int key_blocks;  // blocks of keys of an entry and K/V head at most
   int parts_max;   // row parts at most; 1: sums go straight to the scores
+  int room;        // blocks that the chip holds
   int tiles_max;   // row tiles of an entry and K/V head at most
   int64_t parts;   // few rows: parts of all entries aimed at (of each head)
   char* rows;      // [B Hkv][tiles_max] row tiles as they go to LDS
@@ -32,8 +33,6 @@ struct WeighCut {
   int2* span;      // [B Hkv][tiles_max] the fewest and the most slots that a row of the tile sees
   float* sums;     // [parts_max][B Hkv][cap]
 };
-
-constexpr int kWeighRoom = 512;  // blocks of k_cache_accumulate that the chip holds
 
 // Row parts: the number whose blocks fill the chip a whole number of times best.
 __device__ __forceinline__ int weigh_parts(const CacheCall& c, const WeighCut& w, int keys, int lane) {
@@ -44,7 +43,7 @@ __device__ __forceinline__ int weigh_parts(const CacheCall& c, const WeighCut& w
   used *= c.Hkv;
   int best = 1;
   for (int p = 2; p <= w.parts_max; ++p) {
-    const int64_t now = (used * (int64_t)p + kWeighRoom - 1) / kWeighRoom, was = (used * (int64_t)best + kWeighRoom - 1) / kWeighRoom;
+    const int64_t now = (used * (int64_t)p + w.room - 1) / w.room, was = (used * (int64_t)best + w.room - 1) / w.room;
     if (now * best * 16 < was * p * 15) best = p;
   }
   return best;
@@ -105,18 +104,21 @@ __global__ __launch_bounds__(256) void k_cache_weigh_rows(CacheCall c, WeighCut 
   if (tid == 0) w.span[at] = make_int2(lo, hi);
 }
 
+// Blocks on a CU: three, two where fp32 keys of 512 bytes take the registers.
+constexpr int weigh_blocks(int d, bool bf16) { return d == 128 && !bf16 ? 2 : 3; }
+
 // E: element type; SETS: sets of 32 keys of a wave.
 template <int D, class E, int SETS>
-__global__ __launch_bounds__(256, 2) void k_cache_accumulate(CacheCall c, WeighCut w) {
+__global__ __launch_bounds__(256, weigh_blocks(D, sizeof(E) == 2)) void k_cache_accumulate(CacheCall c, WeighCut w) {
   constexpr int EPC = 16 / sizeof(E);       // elements of a 16-byte chunk
   constexpr int CH = D / EPC, NF = CH / 2;  // chunks of a row; operands of a lane
   constexpr int KEYS = 128 * SETS;          // keys of a block
   constexpr int NCP = 32 * CH / 64;         // 1 KB copies of a tile of rows
   constexpr int CPW = NCP / 4;              // of a wave
   constexpr int NB = 3;
-  __shared__ __attribute__((aligned(1024))) uint4 mem[KEYS * CH];  // keys at first, then NB tiles of rows
+  __shared__ __attribute__((aligned(1024))) uint4 mem[128 * CH];  // sets of keys at first, then NB tiles of rows
   __shared__ float zv[NB][64];
-  static_assert(NB * 32 <= KEYS, "rows fit the keys' memory");
+  static_assert(NB * 32 <= 128, "rows fit the keys' memory");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
@@ -141,18 +143,20 @@ __global__ __launch_bounds__(256, 2) void k_cache_accumulate(CacheCall c, WeighC
     const char* src = (const char*)((const E*)c.k + b * c.sb + hk * c.sh) + (int64_t)key0 * (int64_t)(c.sn * sizeof(E));
     const int left = max(len - 1 - key0, 0);
     const char* base = key0 < len ? src : (const char*)((const E*)c.k + b * c.sb + hk * c.sh);
-    const uint32_t lds = lds_address(mem) + (uint32_t)(wv * 32 * SETS * CH * 16);
+    const uint32_t lds = lds_address(mem) + (uint32_t)(wv * 32 * CH * 16);
+    const uint4* kt = mem + wv * 32 * CH;
 #pragma unroll
-    for (int u = 0; u < NCP * SETS; ++u) {
-      const int s = u * 64 + lane, r = s / CH;
-      g2lds16s(base, (uint32_t)min(r, left) * (uint32_t)(c.sn * sizeof(E)) + (uint32_t)(((s % CH) ^ row_swz<CH>(r & 31)) * 16), lds + u * 1024);
+    for (int s = 0; s < SETS; ++s) {
+#pragma unroll
+      for (int u = 0; u < NCP; ++u) {
+        const int i = u * 64 + lane, r = i / CH;
+        g2lds16s(base, (uint32_t)min(s * 32 + r, left) * (uint32_t)(c.sn * sizeof(E)) + (uint32_t)(((i % CH) ^ row_swz<CH>(r)) * 16), lds + u * 1024);
+      }
+      wait_copies<0>();
+#pragma unroll
+      for (int x = 0; x < NF; ++x) kf[s][x] = kt[n * CH + ((2 * x + h) ^ row_swz<CH>(n))];
+      asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
     }
-    wait_copies<0>();
-    const uint4* kt = mem + wv * 32 * SETS * CH;
-#pragma unroll
-    for (int s = 0; s < SETS; ++s)
-#pragma unroll
-      for (int x = 0; x < NF; ++x) kf[s][x] = kt[(s * 32 + n) * CH + ((2 * x + h) ^ row_swz<CH>(n))];
   }
   float sum[SETS];
 #pragma unroll
@@ -170,7 +174,6 @@ __global__ __launch_bounds__(256, 2) void k_cache_accumulate(CacheCall c, WeighC
       g2lds16s(src, (uint32_t)((u * 4 + wv) * 1024 + lane * 16), q_lds + buf * (32 * CH * 16) + (u * 4 + wv) * 1024);
     if (wv == 0) g2lds4s(w.zv + (tile0 + t) * 64, (uint32_t)lane * 4, z_lds + buf * 256);
   };
-  asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
   __builtin_amdgcn_s_barrier();  // every wave has its keys
   const float sl2 = 1.4426950408889634f / sqrtf((float)D);
   if (t_first < t_last) {
@@ -379,6 +382,7 @@ WeighCut weigh_cut(const CacheCall& c) {
   const int keys = weigh_keys(c.bf16);
   WeighCut w{};
   w.key_blocks = (c.cap + keys - 1) / keys;
+  w.room = 256 * weigh_blocks(c.d, c.bf16);
   w.tiles_max = (int)tiles;
   w.parts_max = (int)std::max<int64_t>(1, std::min<int64_t>(8, tiles / 8));
   return w;

@@ -181,8 +181,14 @@ __global__ __launch_bounds__(256, weigh_blocks(D, sizeof(E) == 2)) void k_cache_
     issue(t_first + 1, 1);
   }
   int buf = 0;
+  // (through the scalar cache: a vector load would wait for the copies behind it)
+  typedef const __attribute__((address_space(4))) int* sptr;
+  auto span_of = [&](int t) {
+    const sptr p = (sptr)(const int*)(w.span + tile0 + __builtin_amdgcn_readfirstlane(t));
+    return make_int2(p[0], p[1]);
+  };
   for (int t = t_first; t < t_last; ++t) {
-    const int2 span = w.span[tile0 + t];
+    const int2 span = span_of(t);
     wait_copies<CPW>();  // this tile's copies are there, the next one's may be under way
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
     __builtin_amdgcn_s_barrier();

@@ -110,6 +110,15 @@ EXPORTED = ["sparsepr_params_default", "sparsepr_workspace_size", "sparsepr_plan
             "sparsepr_cache_accumulate", "sparsepr_cache_evict_workspace_size",
             "sparsepr_cache_evict"]
 
+# argument kinds of the cache operators: p = pointer, i = int32, z = size_t
+CACHE_CALLS = {"sparsepr_cache_attend_workspace_size": "ppp",
+               "sparsepr_cache_attend": "ppppppppppzp",
+               "sparsepr_cache_append": "ppppppippp",
+               "sparsepr_cache_accumulate_workspace_size": "ppip",
+               "sparsepr_cache_accumulate": "pppppippzp",
+               "sparsepr_cache_evict_workspace_size": "pip",
+               "sparsepr_cache_evict": "ppiiipzp"}
+
 _lib = None
 
 
@@ -122,6 +131,9 @@ def lib():
                                "(run __graft_entry__.build() or paper_2608_18484_amd/build.py)")
         L = ctypes.CDLL(LIB_PATH)
         L.sparsepr_last_error.restype = ctypes.c_char_p
+        for name, n_args in CACHE_CALLS.items():  # every argument a pointer or an int
+            getattr(L, name).argtypes = [ctypes.c_int32 if c == "i" else ctypes.c_size_t if c == "z"
+                                         else ctypes.c_void_p for c in n_args]
         for name in EXPORTED:
             if name not in ("sparsepr_last_error", "sparsepr_params_default", "sparsepr_plan_destroy"):
                 getattr(L, name).restype = ctypes.c_int
@@ -395,19 +407,30 @@ def dense_attention(q, k, v, out=None, stream=None):
 
 
 def _tensor(name, t, shape, dtype, device, contiguous=True):
+    """Raises ValueError unless t is a tensor of this shape, dtype and device,
+    contiguous or with a contiguous last dimension."""
     import torch
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
     if t.device != device:
         raise ValueError(f"{name}: tensor on {t.device}, the cache is on {device}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if contiguous and not t.is_contiguous():
+    if t.is_contiguous():
+        return
+    if contiguous:
         raise ValueError(f"{name}: must be contiguous")
-    if not contiguous and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: last dimension must be contiguous")
+
+
+def _same_strides(name, a, other, b):
+    """Strides of dimensions that are stepped over."""
+    if a.stride() != b.stride() and any(n > 1 and x != y for n, x, y in
+                                        zip(a.shape, a.stride(), b.stride())):
+        raise ValueError(f"{name}: strides {a.stride()}, those of {other} are {b.stride()}")
 
 
 def _opt(t):
@@ -442,8 +465,7 @@ class KVCache:
         b, hkv, cap, d = k.shape
         _tensor("k", k, k.shape, k.dtype, k.device, contiguous=False)
         _tensor("v", v, k.shape, k.dtype, k.device, contiguous=False)
-        if any(n > 1 and x != y for n, x, y in zip(k.shape, k.stride(), v.stride())):
-            raise ValueError(f"v: strides {v.stride()}, those of k are {k.stride()}")
+        _same_strides("v", v, "k", k)
         _tensor("lengths", lengths, (b,), torch.int32, k.device)
         if scores is not None:
             _tensor("scores", scores, (b, hkv, cap), torch.float32, k.device)
@@ -456,6 +478,7 @@ class KVCache:
         self.desc = Cache(b, hkv, cap, d, sb, sh, sn, BF16 if k.dtype == torch.bfloat16 else F32,
                           k.data_ptr(), v.data_ptr(), lengths.data_ptr(), _opt(scores),
                           _opt(positions), self._flags.data_ptr())
+        self._desc = ctypes.addressof(self.desc)
 
     _device_type = "cuda"
 
@@ -471,26 +494,27 @@ class KVCache:
 
     # -- marshalling --------------------------------------------------------
 
-    def _on(self, stream):
-        """The stream, and a context that makes it and its device current where
-        they are not, so that scratch memory belongs to the stream that uses it."""
-        import contextlib
-
+    def _run(self, stream, launch):
+        """launch(stream handle), with the stream and the cache's device current
+        where they are not, so that scratch memory and outputs made by the call
+        belong to the stream that uses them."""
         import torch
         if stream is None:
-            s = torch.cuda.current_stream(self.device)
+            handle = torch.cuda.current_stream(self.device).cuda_stream
             if self.device.index == torch.cuda.current_device():
-                return s, contextlib.nullcontext()
-            return s, torch.cuda.device(self.device)
+                return launch(handle)
+            with torch.cuda.device(self.device):
+                return launch(handle)
         if stream.device != self.device:
             raise ValueError(f"stream on {stream.device}, the cache is on {self.device}")
-        return stream, torch.cuda.stream(stream)
+        with torch.cuda.stream(stream):
+            return launch(stream.cuda_stream)
 
     def _scratch(self, size_fn, *args):
         """Scratch memory of one call from torch's allocator (None if it needs none)."""
         import torch
         need = ctypes.c_size_t(0)
-        _check(size_fn(ctypes.byref(self.desc), *args, ctypes.byref(need)))
+        _check(size_fn(self._desc, *args, ctypes.addressof(need)))
         if need.value == 0:
             return None, 0
         return torch.empty(need.value, dtype=torch.uint8, device=self.device), need.value
@@ -500,7 +524,7 @@ class KVCache:
         c = self.desc
         if not isinstance(q, torch.Tensor) or q.dim() != 4:
             raise ValueError("q: expected a [B, H, n, d] torch.Tensor")
-        h, n = q.shape[1], q.shape[2]
+        _, h, n, _ = q.shape
         _tensor("q", q, (c.batch, h, n, c.d), self.dtype, self.device, contiguous=False)
         if n < 1 or h < 1 or h % c.heads_kv != 0:
             raise ValueError(f"q: {h} heads of {n} tokens; heads must be a multiple of the "
@@ -511,8 +535,7 @@ class KVCache:
         c = self.desc
         _tensor("k_new", k_new, (c.batch, c.heads_kv, n, c.d), self.dtype, self.device, False)
         _tensor("v_new", v_new, k_new.shape, self.dtype, self.device, False)
-        if any(m > 1 and x != y for m, x, y in zip(k_new.shape, k_new.stride(), v_new.stride())):
-            raise ValueError(f"v_new: strides {v_new.stride()}, those of k_new are {k_new.stride()}")
+        _same_strides("v_new", v_new, "k_new", k_new)
         return k_new.stride()[:3]
 
     def _list(self, rows, counts, n):
@@ -553,21 +576,23 @@ class KVCache:
             _tensor("out", out, q.shape, self.dtype, self.device, contiguous=False)
         if lse is not None:
             _tensor("lse", lse, (b, h, n), torch.float32, self.device)
-        s, ctx = self._on(stream)
-        with ctx:
+
+        def launch(handle):
+            o, z = out, lse
             make = torch.empty if counts is None else torch.zeros
-            if out is None:
-                out = make(q.shape, dtype=self.dtype, device=self.device)
-            if lse is None:
-                lse = make((b, h, n), dtype=torch.float32, device=self.device)
-            t = Tokens(h, n, *q.stride()[:3], *out.stride()[:3], *ks, mask)
-            L = lib()
-            ws, nbytes = self._scratch(L.sparsepr_cache_attend_workspace_size, ctypes.byref(t))
+            if o is None:
+                o = make(q.shape, dtype=self.dtype, device=self.device)
+            if z is None:
+                z = make((b, h, n), dtype=torch.float32, device=self.device)
+            t = Tokens(h, n, *q.stride()[:3], *o.stride()[:3], *ks, mask)
+            at, L = ctypes.addressof(t), lib()
+            ws, nbytes = self._scratch(L.sparsepr_cache_attend_workspace_size, at)
             _check(L.sparsepr_cache_attend(
-                ctypes.byref(self.desc), ctypes.byref(t), _ptr(q), _ptr(k_new), _ptr(v_new),
-                _P(_opt(parents)), _P(_opt(counts)), _ptr(out), _ptr(lse), _P(_opt(ws)),
-                ctypes.c_size_t(nbytes), _P(s.cuda_stream)))
-        return out, lse
+                self._desc, at, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _opt(parents),
+                _opt(counts), o.data_ptr(), z.data_ptr(), _opt(ws), nbytes, handle))
+            return o, z
+
+        return self._run(stream, launch)
 
     def append(self, k_new, v_new, positions=None, rows=None, counts=None, lengths_out=None,
                stream=None):
@@ -589,13 +614,10 @@ class KVCache:
         if lengths_out is None:
             lengths_out = self.lengths
         _tensor("lengths_out", lengths_out, (c.batch,), torch.int32, self.device)
-        s, ctx = self._on(stream)
-        with ctx:
-            t = Tokens(c.heads_kv, n, 0, 0, 0, 0, 0, 0, *ks, TOKENS_CAUSAL)
-            _check(lib().sparsepr_cache_append(
-                ctypes.byref(c), ctypes.byref(t), _ptr(k_new), _ptr(v_new), _P(_opt(positions)),
-                _P(_opt(rows)), ctypes.c_int32(width), _P(_opt(counts)), _ptr(lengths_out),
-                _P(s.cuda_stream)))
+        t = Tokens(c.heads_kv, n, 0, 0, 0, 0, 0, 0, *ks, TOKENS_CAUSAL)
+        self._run(stream, lambda handle: _check(lib().sparsepr_cache_append(
+            self._desc, ctypes.addressof(t), k_new.data_ptr(), v_new.data_ptr(), _opt(positions),
+            _opt(rows), width, _opt(counts), lengths_out.data_ptr(), handle)))
 
     def accumulate(self, q, lse, rows=None, counts=None, causal=True, stream=None):
         """Add the attention weights of the rows that were just appended (rows
@@ -608,17 +630,17 @@ class KVCache:
         _tensor("lse", lse, (c.batch, h, n), torch.float32, self.device)
         if self.scores is None:
             raise ValueError("accumulate: the cache has no scores")
-        s, ctx = self._on(stream)
-        with ctx:
-            t = Tokens(h, n, *q.stride()[:3], 0, 0, 0, 0, 0, 0,
-                       TOKENS_CAUSAL if causal else TOKENS_FULL)
-            L = lib()
-            ws, nbytes = self._scratch(L.sparsepr_cache_accumulate_workspace_size,
-                                       ctypes.byref(t), ctypes.c_int32(width))
+        t = Tokens(h, n, *q.stride()[:3], 0, 0, 0, 0, 0, 0,
+                   TOKENS_CAUSAL if causal else TOKENS_FULL)
+
+        def launch(handle):
+            at, L = ctypes.addressof(t), lib()
+            ws, nbytes = self._scratch(L.sparsepr_cache_accumulate_workspace_size, at, width)
             _check(L.sparsepr_cache_accumulate(
-                ctypes.byref(c), ctypes.byref(t), _ptr(q), _ptr(lse), _P(_opt(rows)),
-                ctypes.c_int32(width), _P(_opt(counts)), _P(_opt(ws)), ctypes.c_size_t(nbytes),
-                _P(s.cuda_stream)))
+                self._desc, at, q.data_ptr(), lse.data_ptr(), _opt(rows), width, _opt(counts),
+                _opt(ws), nbytes, handle))
+
+        self._run(stream, launch)
 
     def evict(self, budget, n_sink=0, n_recent=0, out=None, stream=None):
         """Keep at most `budget` slots of every K/V head: the first n_sink
@@ -631,12 +653,11 @@ class KVCache:
         for name, x in (("budget", budget), ("n_sink", n_sink), ("n_recent", n_recent)):
             if not 0 <= x < 2 ** 31:
                 raise ValueError(f"{name}: {x} is out of range")
-        s, ctx = self._on(stream)
-        with ctx:
+
+        def launch(handle):
             L = lib()
-            ws, nbytes = self._scratch(L.sparsepr_cache_evict_workspace_size,
-                                       ctypes.c_int32(budget))
-            _check(L.sparsepr_cache_evict(
-                ctypes.byref(self.desc), None if out is None else ctypes.byref(out.desc),
-                ctypes.c_int32(budget), ctypes.c_int32(n_sink), ctypes.c_int32(n_recent),
-                _P(_opt(ws)), ctypes.c_size_t(nbytes), _P(s.cuda_stream)))
+            ws, nbytes = self._scratch(L.sparsepr_cache_evict_workspace_size, budget)
+            _check(L.sparsepr_cache_evict(self._desc, None if out is None else out._desc, budget,
+                                          n_sink, n_recent, _opt(ws), nbytes, handle))
+
+        self._run(stream, launch)

@@ -35,18 +35,18 @@ struct Cut {
   int row_tiles;    // tiles of 32 RS rows of an entry and K/V head
   int ks;           // key tiles of a step
   int split;        // 0: one part per entry
-  int64_t parts;    // split: parts of all entries aimed at (of each head and row tile)
+  int parts;        // split: parts of all entries aimed at (of each head and row tile)
   int slots;        // parts of all entries at most
   float* o;         // [slots][Hkv][T G][D] parts' outputs, relative to their maxima
   float2* ml;       // [slots][Hkv][T G] maxima (base 2) and sums
 };
 
-// Steps of entry b: those of its cache tiles and new tiles together.
-__device__ __forceinline__ int entry_steps(const CacheCall& c, int b, int ks) {
-  const int n = cache_count(c, b, c.T);
-  if (n == 0) return 0;
-  const int tiles = (cache_length(c, b) + kKeys - 1) / kKeys + (n + kKeys - 1) / kKeys;
-  return (tiles + ks - 1) / ks;
+// Steps of an entry: those of its cache tiles and new tiles together.
+__device__ __forceinline__ auto steps_of(const Cut& cut) {
+  return [ks = cut.ks](Entry e) {
+    if (e.n == 0) return 0;
+    return ((e.len + kKeys - 1) / kKeys + (e.n + kKeys - 1) / kKeys + ks - 1) / ks;
+  };
 }
 
 // Every tree token's visible tokens as bits, by doubling: in round i a token
@@ -107,21 +107,20 @@ struct Where {
 // use, the row tiles of a part and head next to each other, which read the
 // same keys.
 __device__ __forceinline__ bool locate(const CacheCall& c, const Cut& cut, int tile_rows, int lane, Where& w) {
-  auto steps = [&](int b) { return entry_steps(c, b, cut.ks); };
-  const int per = cut.split ? part_steps(c.B, cut.parts, lane, steps) : 0x7fffffff;
-  const int64_t used = (int64_t)count_parts(c.B, per, lane, steps) * c.Hkv * cut.row_tiles;
-  const int64_t eighth = (used + 7) / 8;
-  const int64_t at = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
-  if ((int64_t)(blockIdx.x >> 3) >= eighth || at >= used) return false;
-  const int rt = (int)(at % cut.row_tiles), unit = (int)(at / cut.row_tiles);
-  w.hk = unit % c.Hkv;
-  w.slot = unit / c.Hkv;
-  const Part part = find_part(c.B, per, w.slot, lane, steps);
+  const auto all = cut_parts(c, cut.split ? cut.parts : 0, c.T, lane, steps_of(cut));
+  const uint32_t used = (uint32_t)(all.count(c.B) * c.Hkv * cut.row_tiles), eighth = (used + 7) / 8;
+  const uint32_t at = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= eighth || at >= used) return false;
+  const uint32_t unit = at / (uint32_t)cut.row_tiles;
+  const int rt = (int)(at - unit * (uint32_t)cut.row_tiles);
+  w.slot = (int)(unit / (uint32_t)c.Hkv);
+  w.hk = (int)(unit - (uint32_t)w.slot * (uint32_t)c.Hkv);
+  const auto part = all.find(w.slot);
   if (part.b < 0 || w.slot >= cut.slots) return false;  // (only if lengths change during the launch)
   w.b = part.b;
   w.parts = part.count;
-  w.ntok = cache_count(c, w.b, c.T);
-  w.len = cache_length(c, w.b);
+  w.ntok = part.e.n;
+  w.len = part.e.len;
   w.rows = w.ntok * c.G;
   w.row0 = rt * tile_rows;
   if (w.row0 >= w.rows) return false;
@@ -180,7 +179,6 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
   const char* vc = (const char*)((const uint16_t*)c.v + b * c.sb + hk * c.sh);
   const char* kn = (const char*)((const uint16_t*)c.kn + b * c.nsb + hk * c.nsh);
   const char* vn = (const char*)((const uint16_t*)c.vn + b * c.nsb + hk * c.nsh);
-  wait_copies<0>();
 
   // copies of this wave's share of one of key tile i's tensors (0 = K, 1 = V);
   // rows past the end repeat the last one
@@ -641,11 +639,11 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
   const int R = c.T * c.G, tiles = ALONE ? (R + NG - 1) / NG : R;
   const int bh = blockIdx.x / tiles, row = ALONE ? blockIdx.x % tiles * NG + g : blockIdx.x % tiles;
   const int b = bh / c.Hkv, hk = bh % c.Hkv;
-  const int ntok = cache_count(c, b, c.T);
-  auto steps = [&](int e) { return entry_steps(c, e, cut.ks); };
-  const int per = part_steps(c.B, cut.parts, lane, steps);
+  const auto all = cut_parts(c, cut.parts, c.T, lane, steps_of(cut));
   // this entry's parts follow those of the entries before it
-  const int first = count_parts(b, per, lane, steps), count = parts_of(steps(b), per);
+  const int first = all.count(b);
+  const Entry e = b < 64 ? Entry{__shfl(all.own.len, b), __shfl(all.own.n, b)} : all.entry(b);
+  const int ntok = e.n, count = parts_of(all.steps(e), all.per);
   // (one part wrote its rows itself)
   if (count < 2 || row >= ntok * c.G || first + count > cut.slots) return;
   const size_t step = (size_t)c.Hkv * R;
@@ -719,7 +717,9 @@ int row_sets(const CacheCall& c) {
 // B - 1 more, is the most that r rounds hold; more rounds than one where a part
 // is then shorter by a twelfth (a frame's 296 blocks: one part each 566 us, 3
 // parts in two rounds 450, 5 in three 431; 24 blocks: 21 parts 178, 42 in two
-// rounds 187).
+// rounds 187).  Up to 512 keys one part is done before a second kernel would
+// have joined several (one token over 256 slots 12.7 us, in parts 15.8; 512:
+// 15.0 and 16.0; 1,021: 19.2 and 16.0).
 Cut make_cut(const CacheCall& c) {
   Cut cut{};
   const int rs = row_sets(c);
@@ -729,14 +729,14 @@ Cut make_cut(const CacheCall& c) {
   const int64_t units = (int64_t)c.Hkv * cut.row_tiles;  // blocks of a part
   const int64_t room = rs == 1 || (!c.bf16 && c.d == 128) ? 256 : 512;
   double best = 1e30;
-  for (int r = 1; r <= 4; ++r) {
+  for (int r = 1; r <= 4 && (int64_t)c.cap + c.T > 512; ++r) {
     const int64_t parts = r * room / units - (c.B - 1);
     if (parts <= c.B || r / (double)parts >= best * 0.92) continue;
     best = r / (double)parts;
-    cut.parts = parts;
+    cut.parts = (int)parts;
   }
   cut.split = cut.parts > 0;
-  cut.slots = c.B + (cut.split ? (int)cut.parts - 1 : 0);
+  cut.slots = c.B + (cut.split ? cut.parts - 1 : 0);
   return cut;
 }
 

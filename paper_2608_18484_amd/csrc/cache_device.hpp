@@ -22,57 +22,90 @@ __device__ __forceinline__ void raise_flag(const CacheCall& c, int b, int flag) 
 constexpr int kKeys = 32;  // keys of a tile
 
 // The work of a launch, cut into parts of equal length over all entries.  An
-// entry has steps(b) steps, known on the device alone; a part is `per`
-// consecutive ones of an entry (the last part of an entry is shorter), and the
-// parts are numbered in the order of the entries.  All of these are called by
-// whole waves.
-__device__ __forceinline__ int parts_of(int steps, int per) { return steps / per + (steps % per != 0); }
-
-// The length at which all entries together make `parts` parts, and up to B - 1
-// more where they are ragged.
-template <class F>
-__device__ __forceinline__ int part_steps(int B, int64_t parts, int lane, F&& steps) {
-  int64_t total = 0;
-  for (int b0 = 0; b0 < B; b0 += 64) total += wave_sum_i(b0 + lane < B ? steps(b0 + lane) : 0);
-  return (int)max((total + parts - 1) / parts, (int64_t)1);
+// entry has some steps, known on the device alone; a part is `per` consecutive
+// ones of an entry (the last part of an entry is shorter), and the parts are
+// numbered in the order of the entries.  All of this is called by whole waves;
+// up to 64 entries are read once (a lane each), which keeps one trip to memory
+// between the start of a block and its first keys.
+__device__ __forceinline__ int parts_of(int steps, int per) {
+  const uint32_t n = (uint32_t)steps / (uint32_t)per;
+  return (int)(n + (n * (uint32_t)per != (uint32_t)steps));
 }
 
-// Parts of the first B entries.
-template <class F>
-__device__ __forceinline__ int count_parts(int B, int per, int lane, F&& steps) {
-  int used = 0;
-  for (int b0 = 0; b0 < B; b0 += 64) used += wave_sum_i(b0 + lane < B ? parts_of(steps(b0 + lane), per) : 0);
-  return used;
-}
+struct Entry {
+  int len, n;  // slots in use, tokens
+};
 
-struct Part {
-  int b, first, last, count;  // entry (-1: none), its steps [first, last), its parts
+template <class F>
+struct Parts {
+  const CacheCall& c;
+  int most;       // tokens of an entry at most
+  F steps;        // of an Entry
+  int lane;
+  Entry own;      // of entry `lane`
+  int own_steps;
+  int per;        // steps of a part
+
+  __device__ __forceinline__ Entry entry(int b) const { return {cache_length(c, b), cache_count(c, b, most)}; }
+  // steps of entry b0 + lane
+  __device__ __forceinline__ int at(int b0, int B) const {
+    if (b0 == 0) return lane < B ? own_steps : 0;
+    return b0 + lane < B ? steps(entry(b0 + lane)) : 0;
+  }
+
+  // `parts` > 0: the length at which all entries make that many parts, and up to
+  // B - 1 more where they are ragged.  0: one part an entry.
+  __device__ __forceinline__ Parts(const CacheCall& call, int parts, int most_tokens, int lane_, F f)
+      : c(call), most(most_tokens), steps(f), lane(lane_), own{0, 0}, own_steps(0), per(0x7fffffff) {
+    if (lane < c.B) {
+      own = entry(lane);
+      own_steps = steps(own);
+    }
+    if (parts == 0) return;
+    // (K, V and the rows are in memory, so that their tiles' number fits 31 bits)
+    int total = 0;
+    for (int b0 = 0; b0 < c.B; b0 += 64) total += wave_sum_i(at(b0, c.B));
+    per = max(((uint32_t)total + (uint32_t)parts - 1) / (uint32_t)parts, 1u);
+  }
+  // parts of the first B entries
+  __device__ __forceinline__ int count(int B) const {
+    int used = 0;
+    for (int b0 = 0; b0 < B; b0 += 64) used += wave_sum_i(parts_of(at(b0, B), per));
+    return used;
+  }
+  struct Found {
+    int b, first, last, count;  // entry (-1: none), its steps [first, last), its parts
+    Entry e;
+  };
+  __device__ __forceinline__ Found find(int slot) const {
+    Found p{-1, 0, 0, 0, {0, 0}};
+    for (int b0 = 0; b0 < c.B; b0 += 64) {
+      const int st = at(b0, c.B), n = parts_of(st, per);
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(upto, o);
+        if (lane >= o) upto += y;
+      }
+      const uint64_t over = __ballot(upto > slot);
+      if (over) {
+        const int l = __builtin_ctzll(over);
+        const int before = slot - __shfl(upto - n, l), all = __shfl(st, l);
+        p.b = b0 + l;
+        p.count = __shfl(n, l);
+        p.first = (int)min((int64_t)before * per, (int64_t)all);
+        p.last = (int)min((int64_t)(before + 1) * per, (int64_t)all);
+        p.e = b0 == 0 ? Entry{__shfl(own.len, l), __shfl(own.n, l)} : entry(p.b);
+        return p;
+      }
+      slot -= __shfl(upto, 63);
+    }
+    return p;
+  }
 };
 template <class F>
-__device__ __forceinline__ Part find_part(int B, int per, int slot, int lane, F&& steps) {
-  Part p{-1, 0, 0, 0};
-  for (int b0 = 0; b0 < B; b0 += 64) {
-    const int st = b0 + lane < B ? steps(b0 + lane) : 0;
-    const int n = parts_of(st, per);
-    int upto = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(upto, o);
-      if (lane >= o) upto += y;
-    }
-    const uint64_t over = __ballot(upto > slot);
-    if (over) {
-      const int l = __builtin_ctzll(over);
-      const int at = slot - __shfl(upto - n, l), all = __shfl(st, l);
-      p.b = b0 + l;
-      p.count = __shfl(n, l);
-      p.first = (int)min((int64_t)at * per, (int64_t)all);
-      p.last = (int)min((int64_t)(at + 1) * per, (int64_t)all);
-      return p;
-    }
-    slot -= __shfl(upto, 63);
-  }
-  return p;
+__device__ __forceinline__ Parts<F> cut_parts(const CacheCall& c, int parts, int most, int lane, F f) {
+  return Parts<F>(c, parts, most, lane, f);
 }
 
 template <int N>

@@ -27,7 +27,7 @@ struct WeighCut {
   int parts_max;   // row parts at most; 1: sums go straight to the scores
   int room;        // blocks that the chip holds
   int tiles_max;   // row tiles of an entry and K/V head at most
-  int64_t parts;   // few rows: parts of all entries aimed at (of each head)
+  int parts;       // few rows: parts of all entries aimed at (of each head)
   char* rows;      // [B Hkv][tiles_max] row tiles as they go to LDS
   float* zv;       // [B Hkv][tiles_max][2][32] the rows' lse (base 2), and the slots they see
   int2* span;      // [B Hkv][tiles_max] the fewest and the most slots that a row of the tile sees
@@ -125,11 +125,11 @@ __global__ __launch_bounds__(256, weigh_blocks(D, sizeof(E) == 2)) void k_cache_
 
   // XCD x takes the x-th eighth of the blocks: its L2 holds few heads' rows
   const int parts = weigh_parts(c, w, KEYS, lane);
-  const int64_t total = (int64_t)c.B * c.Hkv * parts * w.key_blocks, eighth = (total + 7) / 8;
-  const int64_t at = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
-  if ((int64_t)(blockIdx.x >> 3) >= eighth || at >= total) return;
-  const int kb = (int)(at % w.key_blocks), part = (int)(at / w.key_blocks) % parts;
-  const int bh = (int)(at / w.key_blocks) / parts, b = bh / c.Hkv, hk = bh % c.Hkv;
+  const uint32_t total = (uint32_t)(c.B * c.Hkv) * (uint32_t)(parts * w.key_blocks), eighth = (total + 7) / 8;
+  const uint32_t at = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= eighth || at >= total) return;
+  const int unit = (int)(at / (uint32_t)w.key_blocks), kb = (int)at - unit * w.key_blocks;
+  const int bh = unit / parts, part = unit - bh * parts, b = bh / c.Hkv, hk = bh % c.Hkv;
   const int len = cache_length(c, b), ntok = cache_count(c, b, c.C);
   if (kb * KEYS >= len) return;
   const int tiles = (ntok * c.G + 31) / 32;
@@ -276,12 +276,11 @@ __global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
-  auto steps = [&](int b) { return (cache_length(c, b) + 4 * kKeys - 1) / (4 * kKeys); };
-  const int per = part_steps(c.B, w.parts, lane, steps);
+  const auto all = cut_parts(c, w.parts, c.C, lane, [](Entry e) { return (e.len + 4 * kKeys - 1) / (4 * kKeys); });
   const int slot = blockIdx.x / c.Hkv, hk = blockIdx.x % c.Hkv;
-  const Part part = find_part(c.B, per, slot, lane, steps);
+  const auto part = all.find(slot);
   if (part.b < 0) return;
-  const int b = part.b, len = cache_length(c, b), ntok = cache_count(c, b, c.C);
+  const int b = part.b, len = part.e.len, ntok = part.e.n;
   const int rows = ntok * c.G;
   if (rows == 0) return;
   // this lane's row of the operand; the rows of its score registers
@@ -426,8 +425,8 @@ size_t cache_accumulate_workspace(const CacheCall& c) {
 void launch_cache_accumulate(const CacheCall& c, void* ws, hipStream_t s) {
   WeighCut w = weigh_cut(c);
   if (few_rows(c)) {
-    w.parts = std::max<int64_t>(kRoom / c.Hkv - (c.B - 1), c.B);
-    const dim3 grid((unsigned)((w.parts + c.B - 1) * c.Hkv));
+    w.parts = std::max(kRoom / c.Hkv - (c.B - 1), c.B);
+    const dim3 grid((unsigned)(w.parts + c.B - 1) * (unsigned)c.Hkv);
     if (c.bf16)
       c.d == 64 ? k_cache_weigh_few<64, uint16_t><<<grid, 256, 0, s>>>(c, w) : k_cache_weigh_few<128, uint16_t><<<grid, 256, 0, s>>>(c, w);
     else

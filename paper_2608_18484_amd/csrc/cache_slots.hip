@@ -3,6 +3,7 @@
 #include <limits.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache_device.hpp"
 
@@ -28,28 +29,34 @@ __device__ int rows_to_append(const CacheCall& c, int b, int len, int& flag) {
 }
 
 // Rows of new K and V into the slots behind the used ones, 16 bytes a thread.
-__global__ __launch_bounds__(256) void k_cache_append(CacheCall c, const int32_t* tpos, int32_t* lengths_out) {
-  const int bh = blockIdx.y, b = bh / c.Hkv, hk = bh % c.Hkv;
+// `whole`: a block takes all of an entry's; then it is the only one that reads the
+// entry's length and may write it in place.
+__global__ __launch_bounds__(256) void k_cache_append(CacheCall c, const int32_t* tpos, int32_t* lengths_out, int whole) {
+  const int b = whole ? blockIdx.y : blockIdx.y / c.Hkv, h0 = whole ? 0 : blockIdx.y % c.Hkv, heads = whole ? c.Hkv : 1;
   const int es = c.bf16 ? 2 : 4, ch = c.d * es / 16;
   const int len = cache_length(c, b);
   int flag;
   const int n = rows_to_append(c, b, len, flag);
-  if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) {
+  if (blockIdx.x == 0 && h0 == 0 && threadIdx.x == 0) {
     if (flag) raise_flag(c, b, flag);
-    if (lengths_out != c.lengths) lengths_out[b] = len + max(n, 0);
+    if (lengths_out != c.lengths || whole) lengths_out[b] = len + max(n, 0);
   }
-  const int i = (blockIdx.x * 256 + threadIdx.x) / ch, part = (blockIdx.x * 256 + threadIdx.x) % ch;
-  if (i >= n) return;
-  const int r = c.rows ? c.rows[(size_t)b * c.C + i] : i;
-  const int64_t src = (b * c.nsb + hk * c.nsh + (int64_t)r * c.nsn) * es + part * 16;
-  const int64_t dst = (b * c.sb + hk * c.sh + (int64_t)(len + i) * c.sn) * es + part * 16;
-  const uint4 kv = *(const uint4*)((const char*)c.kn + src), vv = *(const uint4*)((const char*)c.vn + src);
-  *(uint4*)((char*)const_cast<void*>(c.k) + dst) = kv;
-  *(uint4*)((char*)const_cast<void*>(c.v) + dst) = vv;
-  if (part == 0) {
-    const size_t slot = (size_t)bh * c.cap + len + i;
-    if (c.scores) c.scores[slot] = 0.f;
-    if (c.positions) c.positions[slot] = tpos[(size_t)b * c.T + r];
+  const int64_t per = (int64_t)n * ch;
+  for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < per * heads; x += (int64_t)gridDim.x * 256) {
+    const int hk = h0 + (whole ? (int)(x / per) : 0);
+    const int64_t y = whole ? x % per : x;
+    const int i = (int)(y / ch), part = (int)(y % ch);
+    const int r = c.rows ? c.rows[(size_t)b * c.C + i] : i;
+    const int64_t src = (b * c.nsb + hk * c.nsh + (int64_t)r * c.nsn) * es + part * 16;
+    const int64_t dst = (b * c.sb + hk * c.sh + (int64_t)(len + i) * c.sn) * es + part * 16;
+    const uint4 kv = *(const uint4*)((const char*)c.kn + src), vv = *(const uint4*)((const char*)c.vn + src);
+    *(uint4*)((char*)const_cast<void*>(c.k) + dst) = kv;
+    *(uint4*)((char*)const_cast<void*>(c.v) + dst) = vv;
+    if (part == 0) {
+      const size_t slot = ((size_t)b * c.Hkv + hk) * c.cap + len + i;
+      if (c.scores) c.scores[slot] = 0.f;
+      if (c.positions) c.positions[slot] = tpos[(size_t)b * c.T + r];
+    }
   }
 }
 
@@ -63,17 +70,25 @@ __global__ __launch_bounds__(256) void k_cache_append_lengths(CacheCall c) {
 
 // ---- eviction ---------------------------------------------------------------
 
-// Workspace of an eviction: per K/V head (rows to move, rows kept), the freed
-// slots and the slots that move into them, for another cache the source of
-// every kept slot, and the slots' keys.
+// Workspace of an eviction, per K/V head.
 struct EvictWork {
-  int2* count;
-  int32_t* hole;   // [budget]
-  int32_t* mover;  // [budget]
-  int32_t* src;    // [budget]
-  uint32_t* key;   // [cap_pad]
-  int cap_pad;     // capacity rounded up to 4
+  uint32_t* key;   // [cap_pad] the slots' keys
+  int2* count;     // rows to move, rows kept
+  int32_t* hole;   // [budget] freed slots below the budget
+  int32_t* mover;  // [budget] kept slots behind it
+  int32_t* stay;   // [budget] for another cache: the slot itself, ~i where it is the i-th freed
+  // large caches
+  int32_t* hist;    // [kBins] slots by the first digit of their key
+  int32_t* newest;  // [blocks] largest position of a block's slots
+  int2* part;       // [blocks] (freed, moving) slots of a block, then those before it
+  uint2* cand;      // [cap_pad] (key, slot) of the slots that the first digit does not decide
+  int4* state;      // their number; the least key that stays; the last slot that stays with it
+  int cap_pad;      // capacity rounded up to 4
+  int blocks;       // of kSlots slots
 };
+
+constexpr int kBins = 2048;   // of a digit: 11 bits
+constexpr int kSlots = 4096;  // slots of a block of the large caches' kernels
 
 // A slot's rank: larger keys stay.  Every slot's key is at least that of -inf,
 // so 0 stands for no slot.
@@ -84,6 +99,69 @@ __device__ __forceinline__ uint32_t evict_key(float score, int pos, bool by_pos,
 }
 
 typedef int32_t i32x4_u __attribute__((ext_vector_type(4), aligned(4)));
+
+// Four neighbours from slot j; those past the end repeat the last slot.
+__device__ __forceinline__ i32x4_u four(const int32_t* p, int j, int len) {
+  i32x4_u v;
+  if (j + 4 <= len) {
+    v = *(const i32x4_u*)(p + j);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = p[min(j + e, len - 1)];
+  }
+  return v;
+}
+
+// A histogram of a digit in LDS, in copies so that equal digits of neighbouring
+// lanes do not meet.
+constexpr int kCopies = 4;
+struct Hist {
+  int bin[kBins][kCopies];
+  int wsum[16], digit, need, same;
+};
+__device__ __forceinline__ void hist_clear(Hist& h) {
+  for (int x = threadIdx.x; x < kBins; x += blockDim.x) *(int4*)h.bin[x] = make_int4(0, 0, 0, 0);
+  __syncthreads();
+}
+// Four more keys of a lane, those that are `on`; where all of a wave's have one
+// digit (protected slots, slots that nothing has weighed yet), one addition.
+__device__ __forceinline__ void hist_add(Hist& h, const bool* on, const int* digit, int lane) {
+  const int first = __builtin_amdgcn_readfirstlane(digit[0]);
+  const bool one = on[0] && on[1] && on[2] && on[3] && digit[0] == first && digit[1] == first && digit[2] == first && digit[3] == first;
+  if (__ballot(one) == ~0ull) {
+    if (lane == 0) atomicAdd(&h.bin[first][0], 256);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (on[e]) atomicAdd(&h.bin[digit[e]][lane & (kCopies - 1)], 1);
+}
+// The digit at which the count from the top reaches `need` (h.digit), how many
+// of its keys are then needed (h.need) and how many there are (h.same).  Thread t
+// of 1024 has the counts hi and lo of the digits 2047 - 2 t and 2046 - 2 t.
+__device__ __forceinline__ void hist_find(Hist& h, int hi, int lo, int need) {
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, own = hi + lo;
+  int upto = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 63) h.wsum[wv] = upto;
+  __syncthreads();
+  for (int x = 0; x < wv; ++x) upto += h.wsum[x];
+  if (upto >= need && upto - own < need) {
+    const int left = need - (upto - own);
+    h.digit = left <= hi ? kBins - 1 - 2 * tid : kBins - 2 - 2 * tid;
+    h.need = left <= hi ? left : left - hi;
+    h.same = left <= hi ? hi : lo;
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ int bin_of(const Hist& h, int x) {
+  const int4 v = *(const int4*)h.bin[x];
+  return v.x + v.y + v.z + v.w;
+}
 
 // One block a K/V head: the budget-th largest key by digits of 11, 11 and 10
 // bits, then the freed and the moving slots numbered in their order.
@@ -96,9 +174,8 @@ typedef int32_t i32x4_u __attribute__((ext_vector_type(4), aligned(4)));
 // with loads of 4 bytes a pass over 75,606 slots took 10 us, keys kept in 80
 // registers a lane instead made 100 KB of code that every launch fetches anew.
 __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w, int in_place, int budget, int n_sink, int n_recent) {
-  constexpr int BINS = 2048, COPIES = 4;  // of the histogram: equal digits of neighbouring lanes do not meet
-  __shared__ int hist[BINS][COPIES];
-  __shared__ int wsum[3][16], sh_digit, sh_need, sh_same, sh_newest;
+  __shared__ Hist hist;
+  __shared__ int wsum[3][16], sh_newest;
   const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = cache_length(c, bh / c.Hkv);
@@ -108,27 +185,16 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
   uint32_t* key = w.key + (size_t)bh * w.cap_pad;
   int32_t* hole = w.hole + (size_t)bh * budget;
   int32_t* mover = w.mover + (size_t)bh * budget;
-  int32_t* src = w.src + (size_t)bh * budget;
+  int32_t* stay = w.stay + (size_t)bh * budget;
   if (len <= budget) {
     if (!in_place)
-      for (int j = tid; j < len; j += 1024) src[j] = j;
+      for (int j = tid; j < len; j += 1024) stay[j] = j;
     if (tid == 0) w.count[bh] = make_int2(0, len);
     return;
   }
   constexpr int AHEAD = 4;
   const int turns = (len + 4095) / 4096;  // of a wave, 256 slots each
   const int j0 = wv * turns * 256 + lane * 4;
-  // four neighbours from slot j; those past the end repeat the last slot
-  auto four = [&](const int32_t* p, int j) {
-    i32x4_u v;
-    if (j + 4 <= len) {
-      v = *(const i32x4_u*)(p + j);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = p[min(j + e, len - 1)];
-    }
-    return v;
-  };
   int newest = INT_MIN;
   if (n_recent > 0) {
     if (tid == 0) sh_newest = INT_MIN;
@@ -136,7 +202,7 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
     for (int i = 0; i < turns; i += AHEAD) {
       i32x4_u v[AHEAD];
 #pragma unroll
-      for (int x = 0; x < AHEAD; ++x) v[x] = four(pos, j0 + min(i + x, turns - 1) * 256);
+      for (int x = 0; x < AHEAD; ++x) v[x] = four(pos, j0 + min(i + x, turns - 1) * 256, len);
 #pragma unroll
       for (int x = 0; x < AHEAD; ++x) newest = max(newest, max(max(v[x].x, v[x].y), max(v[x].z, v[x].w)));
     }
@@ -146,20 +212,6 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
     __syncthreads();
     newest = sh_newest;
   }
-  // four more keys of a lane in the histogram, those that are `on`; where all of
-  // a wave's have one digit (protected slots, slots that nothing has weighed
-  // yet), one addition
-  auto count = [&](const bool* on, const int* digit) {
-    const int first = __builtin_amdgcn_readfirstlane(digit[0]);
-    const bool one = on[0] && on[1] && on[2] && on[3] && digit[0] == first && digit[1] == first && digit[2] == first && digit[3] == first;
-    if (__ballot(one) == ~0ull) {
-      if (lane == 0) atomicAdd(&hist[first][0], 256);
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (on[e]) atomicAdd(&hist[digit[e]][lane & (COPIES - 1)], 1);
-  };
   // f(slot of the lane's first key, keys), in the order of the slots; every
   // lane of a wave takes part
   auto each = [&](auto&& f) {
@@ -178,8 +230,7 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
   uint32_t prefix = 0, mask = 0;
   int need = budget, same = 0;  // keys still to take among those that match the prefix; those
   for (int shift = 21; shift >= 0; shift = shift > 10 ? 10 : shift > 0 ? 0 : -1) {
-    for (int x = tid; x < BINS * COPIES; x += 1024) (&hist[0][0])[x] = 0;
-    __syncthreads();
+    hist_clear(hist);
     const int dmask = shift == 0 ? 1023 : 2047;
     if (shift == 21) {
       for (int i = 0; i < turns; i += AHEAD) {
@@ -187,8 +238,8 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x) {
           const int j = j0 + min(i + x, turns - 1) * 256;
-          s[x] = four((const int32_t*)score, j);
-          if (by_pos) p[x] = four(pos, j);
+          s[x] = four((const int32_t*)score, j, len);
+          if (by_pos) p[x] = four(pos, j, len);
         }
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x) {
@@ -204,7 +255,7 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
             on[e] = j + e < len;
             digit[e] = (int)(k[e] >> 21);
           }
-          count(on, digit);
+          hist_add(hist, on, digit, lane);
           if (j < len) *(uint4*)(key + j) = make_uint4(k[0], k[1], k[2], k[3]);
         }
       }
@@ -219,33 +270,14 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
           digit[e] = (int)(k[e] >> shift) & dmask;
           any |= on[e];
         }
-        if (__ballot(any)) count(on, digit);
+        if (__ballot(any)) hist_add(hist, on, digit, lane);
       });
     }
     __syncthreads();
-    // thread t has the digits 2047 - 2 t and 2046 - 2 t; the one where the sum
-    // from the top reaches `need` is the next of the prefix
-    const int4 h1 = *(const int4*)hist[BINS - 1 - 2 * tid], h0 = *(const int4*)hist[BINS - 2 - 2 * tid];
-    const int hi = h1.x + h1.y + h1.z + h1.w, own = hi + h0.x + h0.y + h0.z + h0.w;
-    int upto = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(upto, o);
-      if (lane >= o) upto += y;
-    }
-    if (lane == 63) wsum[0][wv] = upto;
-    __syncthreads();
-    for (int x = 0; x < wv; ++x) upto += wsum[0][x];
-    if (upto >= need && upto - own < need) {
-      const int left = need - (upto - own);
-      sh_digit = left <= hi ? BINS - 1 - 2 * tid : BINS - 2 - 2 * tid;
-      sh_need = left <= hi ? left : left - hi;
-      sh_same = left <= hi ? hi : own - hi;
-    }
-    __syncthreads();
-    need = sh_need;
-    same = sh_same;
-    prefix |= (uint32_t)sh_digit << shift;
+    hist_find(hist, bin_of(hist, kBins - 1 - 2 * tid), bin_of(hist, kBins - 2 - 2 * tid), need);
+    need = hist.need;
+    same = hist.same;
+    prefix |= (uint32_t)hist.digit << shift;
     mask |= (uint32_t)dmask << shift;
     if (same == need) break;  // all that match stay: the lower digits do not matter
   }
@@ -323,29 +355,283 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
     for (int e = 0; e < 4; ++e) {
       if (freed[e]) hole[rf++] = j + e;
       if (moves[e]) mover[rm++] = j + e;
-      if (!in_place && !freed[e] && j + e < budget) src[j + e] = j + e;
+      if (!in_place && j + e < budget) stay[j + e] = freed[e] ? ~(rf - 1) : j + e;
     }
     at_hole += total(bf);
     at_move += total(bm);
   });
-  if (!in_place) {
-    __syncthreads();
-    for (int r = tid; r < moves_all; r += 1024) src[hole[r]] = mover[r];
-  }
   if (tid == 0) w.count[bh] = make_int2(moves_all, budget);
 }
 
-// The kept rows to their slots, 16 bytes of K and of V a thread.
+// Large caches, a block for every 4,096 slots.  First the newest position of
+// each block's slots; the head's histogram is cleared.
+__global__ __launch_bounds__(1024) void k_evict_newest(CacheCall c, EvictWork w, int budget, int n_recent) {
+  __shared__ int best[16];
+  const int bh = blockIdx.x / w.blocks, blk = blockIdx.x % w.blocks, tid = threadIdx.x;
+  const int len = cache_length(c, bh / c.Hkv), j = blk * kSlots + tid * 4;
+  for (int x = blk * 1024 + tid; x < kBins; x += w.blocks * 1024) w.hist[(size_t)bh * kBins + x] = 0;
+  if (blk == 0 && tid == 0) w.state[bh] = make_int4(0, 0, 0, 0);
+  if (n_recent == 0 || len <= budget || blk * kSlots >= len) return;
+  int m = INT_MIN;
+  if (j < len) {
+    const i32x4_u p = four(c.positions + (size_t)bh * c.cap, j, len);
+    m = max(max(p.x, p.y), max(p.z, p.w));
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o));
+  if ((tid & 63) == 0) best[tid >> 6] = m;
+  __syncthreads();
+  if (tid > 0) return;
+  for (int x = 1; x < 16; ++x) m = max(m, best[x]);
+  w.newest[(size_t)bh * w.blocks + blk] = m;
+}
+
+// The keys, and the head's histogram of their first digits.
+__global__ __launch_bounds__(1024) void k_evict_keys(CacheCall c, EvictWork w, int budget, int n_sink, int n_recent) {
+  __shared__ Hist hist;
+  const int bh = blockIdx.x / w.blocks, blk = blockIdx.x % w.blocks, tid = threadIdx.x, lane = tid & 63;
+  const int len = cache_length(c, bh / c.Hkv), j = blk * kSlots + tid * 4;
+  if (len <= budget || blk * kSlots >= len) return;
+  const bool by_pos = n_sink > 0 || n_recent > 0;
+  i32x4_u s{}, p{};
+  if (j < len) {
+    s = four((const int32_t*)c.scores + (size_t)bh * c.cap, j, len);
+    if (by_pos) p = four(c.positions + (size_t)bh * c.cap, j, len);
+  }
+  int newest = INT_MIN;
+  if (n_recent > 0) {
+    for (int x = lane; x * kSlots < len; x += 64) newest = max(newest, w.newest[(size_t)bh * w.blocks + x]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) newest = max(newest, __shfl_xor(newest, o));
+  }
+  hist_clear(hist);
+  uint32_t k[4];
+  bool on[4];
+  int digit[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    on[e] = j + e < len;
+    k[e] = on[e] ? evict_key(__int_as_float(s[e]), p[e], by_pos, n_sink, n_recent, newest) : 0;
+    digit[e] = (int)(k[e] >> 21);
+  }
+  hist_add(hist, on, digit, lane);
+  if (j < len) *(uint4*)(w.key + (size_t)bh * w.cap_pad + j) = make_uint4(k[0], k[1], k[2], k[3]);
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int n = bin_of(hist, tid * 2 + x);
+    if (n) atomicAdd(&w.hist[(size_t)bh * kBins + tid * 2 + x], n);
+  }
+}
+
+__device__ __forceinline__ void head_find(const EvictWork& w, int bh, Hist& hist, int budget) {
+  const int2 lohi = *(const int2*)(w.hist + (size_t)bh * kBins + kBins - 2 - 2 * threadIdx.x);
+  hist_find(hist, lohi.y, lohi.x, budget);
+}
+
+__device__ __forceinline__ uint4 block_keys(const EvictWork& w, int bh, int j, int len) {
+  return j < len ? *(const uint4*)(w.key + (size_t)bh * w.cap_pad + j) : make_uint4(0, 0, 0, 0);
+}
+
+// The slots that the first digit decides are counted, the others listed.
+__global__ __launch_bounds__(1024) void k_evict_list(CacheCall c, EvictWork w, int budget) {
+  __shared__ Hist hist;
+  __shared__ int freed[16], moving[16], listed[16], at;
+  const int bh = blockIdx.x / w.blocks, blk = blockIdx.x % w.blocks, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int len = cache_length(c, bh / c.Hkv), j = blk * kSlots + tid * 4;
+  if (len <= budget || blk * kSlots >= len) return;
+  const uint4 k4 = block_keys(w, bh, j, len);
+  head_find(w, bh, hist, budget);
+  const int digit = hist.digit;
+  const bool open = hist.same > hist.need;  // of the digit's slots, some go
+  const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+  int nf = 0, nm = 0, nl = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int d = (int)(k[e] >> 21);
+    const bool in = j + e < len, mine = in && open && d == digit;
+    nl += mine;
+    nf += in && !mine && d < digit && j + e < budget;
+    nm += in && !mine && d >= digit && j + e >= budget;
+  }
+  // (a slot past the end has digit 0 and is none of these)
+  int upto = nl;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(upto, o);
+    if (lane >= o) upto += y;
+  }
+  nf = wave_sum_i(nf);
+  nm = wave_sum_i(nm);
+  if (lane == 0) freed[wv] = nf, moving[wv] = nm;
+  if (lane == 63) listed[wv] = upto;
+  __syncthreads();
+  if (tid == 0) {
+    int f = 0, m = 0, l = 0;
+    for (int x = 0; x < 16; ++x) f += freed[x], m += moving[x], l += listed[x];
+    w.part[(size_t)bh * w.blocks + blk] = make_int2(f, m);
+    at = l ? atomicAdd(&w.state[bh].x, l) : 0;
+  }
+  __syncthreads();
+  int put = at + upto - nl;
+  for (int x = 0; x < wv; ++x) put += listed[x];
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (j + e < len && open && (int)(k[e] >> 21) == digit) w.cand[(size_t)bh * w.cap_pad + put++] = make_uint2(k[e], (uint32_t)(j + e));
+}
+
+// One block a head: which of the listed slots stay (by the key's other digits,
+// of equal keys the lowest slots), and the freed and moving slots before each
+// block.  The list's order does not matter.
+__global__ __launch_bounds__(1024) void k_evict_settle(CacheCall c, EvictWork w, int budget) {
+  __shared__ Hist hist;
+  __shared__ int wsum[2][16];
+  const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int len = cache_length(c, bh / c.Hkv);
+  if (len <= budget) {
+    if (tid == 0) w.count[bh] = make_int2(0, len);
+    return;
+  }
+  const uint2* cand = w.cand + (size_t)bh * w.cap_pad;
+  const int n = w.state[bh].x, blocks = (len + kSlots - 1) / kSlots;
+  head_find(w, bh, hist, budget);
+  uint32_t least = (uint32_t)hist.digit << 21, mask = 2047u << 21;
+  int need = hist.need, same = hist.same, last = INT_MAX;
+  // two more digits of the key, then three of the slot: those that a list is
+  // matched by so far
+  uint32_t slot_at = 0, slot_mask = 0;
+  for (int pass = 0; pass < 5 && same > need; ++pass) {
+    const bool by_slot = pass >= 2;
+    const int shift = pass == 0 ? 10 : pass == 1 ? 0 : pass == 2 ? 18 : pass == 3 ? 7 : 0;
+    const uint32_t dmask = pass == 1 ? 1023u : pass == 4 ? 127u : 2047u;
+    __syncthreads();
+    hist_clear(hist);
+    for (int i = tid; i < n; i += 1024) {
+      const uint2 x = cand[i];
+      if ((x.x & mask) != least || (x.y & slot_mask) != slot_at) continue;
+      // slots count from the lowest: their digits are turned round
+      const uint32_t d = by_slot ? dmask - ((x.y >> shift) & dmask) : (x.x >> shift) & dmask;
+      atomicAdd(&hist.bin[d][lane & (kCopies - 1)], 1);
+    }
+    __syncthreads();
+    hist_find(hist, bin_of(hist, kBins - 1 - 2 * tid), bin_of(hist, kBins - 2 - 2 * tid), need);
+    need = hist.need;
+    same = hist.same;
+    if (!by_slot) {
+      least |= (uint32_t)hist.digit << shift;
+      mask |= dmask << shift;
+    } else {
+      slot_at |= (dmask - (uint32_t)hist.digit) << shift;
+      slot_mask |= dmask << shift;
+    }
+  }
+  // keys above `least` in the digits of `mask` stay, and of those that equal it
+  // all, or the slots up to the last that the slot's digits tell
+  if (slot_mask) last = (int)(slot_at | (~slot_mask & 0x1fffffffu));
+  __syncthreads();
+  // exclusive sums over the blocks, 1,024 at a time, the listed slots among them
+  int2* part = w.part + (size_t)bh * w.blocks;
+  int base_f = 0, base_m = 0;
+  for (int x0 = 0; x0 < blocks; x0 += 1024) {
+    const int x = x0 + tid;
+    int2 own = make_int2(0, 0);
+    if (x < blocks) own = part[x];
+    hist.bin[tid][0] = 0;
+    hist.bin[tid][1] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += 1024) {
+      const uint2 v = cand[i];
+      const uint32_t k = v.x & mask;
+      const int s = (int)v.y, at = s / kSlots - x0;
+      const bool keep = k > least || (k == least && s <= last);
+      if (at < 0 || at >= 1024) continue;
+      if (keep && s >= budget) atomicAdd(&hist.bin[at][1], 1);
+      if (!keep && s < budget) atomicAdd(&hist.bin[at][0], 1);
+    }
+    __syncthreads();
+    const int f = own.x + hist.bin[tid][0], m = own.y + hist.bin[tid][1];
+    int uf = f, um = m;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int yf = __shfl_up(uf, o), ym = __shfl_up(um, o);
+      if (lane >= o) uf += yf, um += ym;
+    }
+    if (lane == 63) wsum[0][wv] = uf, wsum[1][wv] = um;
+    __syncthreads();
+    int af = base_f + uf - f, am = base_m + um - m;
+    for (int y = 0; y < 16; ++y) {
+      if (y < wv) af += wsum[0][y], am += wsum[1][y];
+      base_f += wsum[0][y];
+      base_m += wsum[1][y];
+    }
+    if (x < blocks) part[x] = make_int2(af, am);
+    __syncthreads();
+  }
+  if (tid == 0) {
+    w.count[bh] = make_int2(base_m, budget);
+    w.state[bh] = make_int4(n, (int)least, last, (int)mask);
+  }
+}
+
+// The freed and the moving slots at their places.
+__global__ __launch_bounds__(1024) void k_evict_number(CacheCall c, EvictWork w, int in_place, int budget) {
+  __shared__ int freed[16], moving[16];
+  const int bh = blockIdx.x / w.blocks, blk = blockIdx.x % w.blocks, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int len = cache_length(c, bh / c.Hkv), j = blk * kSlots + tid * 4;
+  if (blk * kSlots >= len) return;
+  int32_t* stay = w.stay + (size_t)bh * budget;
+  if (len <= budget) {
+    if (!in_place)
+      for (int e = 0; e < 4; ++e)
+        if (j + e < len) stay[j + e] = j + e;
+    return;
+  }
+  const uint4 k4 = block_keys(w, bh, j, len);
+  const int4 st = w.state[bh];
+  const int2 base = w.part[(size_t)bh * w.blocks + blk];
+  const uint32_t least = (uint32_t)st.y, mask = (uint32_t)st.w, k[4] = {k4.x & mask, k4.y & mask, k4.z & mask, k4.w & mask};
+  bool f[4], m[4];
+  int nf = 0, nm = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool in = j + e < len, keep = in && (k[e] > least || (k[e] == least && j + e <= st.z));
+    f[e] = in && !keep && j + e < budget;
+    m[e] = keep && j + e >= budget;
+    nf += f[e];
+    nm += m[e];
+  }
+  int uf = nf, um = nm;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int yf = __shfl_up(uf, o), ym = __shfl_up(um, o);
+    if (lane >= o) uf += yf, um += ym;
+  }
+  if (lane == 63) freed[wv] = uf, moving[wv] = um;
+  __syncthreads();
+  int af = base.x + uf - nf, am = base.y + um - nm;
+  for (int x = 0; x < wv; ++x) af += freed[x], am += moving[x];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (f[e]) w.hole[(size_t)bh * budget + af++] = j + e;
+    if (m[e]) w.mover[(size_t)bh * budget + am++] = j + e;
+    if (!in_place && j + e < budget) stay[j + e] = f[e] ? ~(af - 1) : j + e;
+  }
+}
+
+// The kept rows to their slots, 16 bytes of K and of V a thread: those that
+// move, or for another cache all of them.
 __global__ __launch_bounds__(256) void k_evict_move(CacheCall c, EvictTo to, EvictWork w, int budget) {
   const int bh = blockIdx.y, b = bh / c.Hkv, hk = bh % c.Hkv;
   const int es = c.bf16 ? 2 : 4, ch = c.d * es / 16;
   const int2 cnt = w.count[bh];
   const int n = to.in_place ? cnt.x : cnt.y;
+  const size_t base = (size_t)bh * budget;
   if (hk == 0 && blockIdx.x == 0 && threadIdx.x == 0) to.lengths[b] = cnt.y;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * ch; i += (int64_t)gridDim.x * 256) {
     const int r = (int)(i / ch), part = (int)(i % ch);
-    const int dst = to.in_place ? w.hole[(size_t)bh * budget + r] : r;
-    const int src = (to.in_place ? w.mover : w.src)[(size_t)bh * budget + r];
+    const int dst = to.in_place ? w.hole[base + r] : r;
+    const int own = to.in_place ? ~r : w.stay[base + r];
+    const int src = own >= 0 ? own : w.mover[base + ~own];
     const int64_t so = (b * c.sb + hk * c.sh + (int64_t)src * c.sn) * es + part * 16;
     const int64_t po = (b * to.sb + hk * to.sh + (int64_t)dst * to.sn) * es + part * 16;
     const uint4 kv = *(const uint4*)((const char*)c.k + so), vv = *(const uint4*)((const char*)c.v + so);
@@ -358,13 +644,34 @@ __global__ __launch_bounds__(256) void k_evict_move(CacheCall c, EvictTo to, Evi
   }
 }
 
-EvictWork evict_work(const CacheCall& c, int budget, void* ws) {
+// Beyond 24,576 slots a head's slots are shared by several blocks, in five
+// launches: 75,600 slots of 16 heads 39 us with an append, one block a head 51;
+// 32,000 slots of 8 heads cut to 4,000 43 and 49; but 17,160 of 32 heads 63 and
+// 57, 9,000 of 8 heads 40 and 28.
+bool evict_large(const CacheCall& c) { return c.cap > 24576; }
+
+// The workspace's arrays in their order (ws null: their bytes alone).
+size_t evict_layout(const CacheCall& c, int budget, void* ws, EvictWork& w) {
   const size_t n = (size_t)c.B * c.Hkv;
-  const int pad = (c.cap + 3) / 4 * 4;
-  uint32_t* key = (uint32_t*)ws;  // first: it is read by 16 bytes
-  int2* count = (int2*)(key + n * pad);
-  int32_t* p = (int32_t*)(count + n);
-  return {count, p, p + n * budget, p + 2 * n * budget, key, pad};
+  w.cap_pad = (c.cap + 3) / 4 * 4;
+  w.blocks = (c.cap + kSlots - 1) / kSlots;
+  size_t at = 0;
+  auto take = [&](auto*& p, size_t per_head) {
+    p = (std::remove_reference_t<decltype(p)>)((char*)ws + at);
+    at += (n * per_head * sizeof(*p) + 15) / 16 * 16;
+  };
+  take(w.key, w.cap_pad);
+  take(w.count, 1);
+  take(w.hole, budget);
+  take(w.mover, budget);
+  take(w.stay, budget);
+  if (!evict_large(c)) return at;
+  take(w.hist, kBins);
+  take(w.newest, w.blocks);
+  take(w.part, w.blocks);
+  take(w.cand, w.cap_pad);
+  take(w.state, 1);
+  return at;
 }
 
 }  // namespace
@@ -372,23 +679,42 @@ EvictWork evict_work(const CacheCall& c, int budget, void* ws) {
 void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int32_t* lengths_out,
                          hipStream_t s) {
   const int ch = c.d * (c.bf16 ? 2 : 4) / 16;
-  const unsigned blocks = (unsigned)(((int64_t)c.C * ch + 255) / 256);
-  k_cache_append<<<dim3(blocks, c.B * c.Hkv), 256, 0, s>>>(c, token_positions, lengths_out);
-  if (lengths_out == c.lengths) k_cache_append_lengths<<<c.B, 256, 0, s>>>(c);
+  const int64_t chunks = (int64_t)c.C * ch;
+  // lengths in place: few rows in one launch (up to eight turns of a block),
+  // more of them with the lengths in a launch of their own
+  const bool in_place = lengths_out == c.lengths;
+  if (in_place && chunks * c.Hkv <= 2048) {
+    k_cache_append<<<dim3(1, c.B), 256, 0, s>>>(c, token_positions, lengths_out, 1);
+    return;
+  }
+  k_cache_append<<<dim3((unsigned)((chunks + 255) / 256), c.B * c.Hkv), 256, 0, s>>>(c, token_positions, lengths_out, 0);
+  if (in_place) k_cache_append_lengths<<<c.B, 256, 0, s>>>(c);
 }
 
 size_t cache_evict_workspace(const CacheCall& c, int budget) {
-  return (size_t)c.B * c.Hkv * (8 + 12 * (size_t)budget + 4 * (size_t)((c.cap + 3) / 4 * 4));
+  EvictWork w{};
+  return evict_layout(c, budget, nullptr, w);
 }
 
 void launch_cache_evict(const CacheCall& c, const EvictTo& to, int budget, int n_sink,
                         int n_recent, void* ws, hipStream_t s) {
-  const EvictWork w = evict_work(c, budget, ws);
-  k_evict_select<<<c.B * c.Hkv, 1024, 0, s>>>(c, w, to.in_place, budget, n_sink, n_recent);
+  EvictWork w{};
+  (void)evict_layout(c, budget, ws, w);
+  const int heads = c.B * c.Hkv;
+  if (evict_large(c)) {
+    const unsigned blocks = (unsigned)heads * (unsigned)w.blocks;
+    k_evict_newest<<<blocks, 1024, 0, s>>>(c, w, budget, n_recent);
+    k_evict_keys<<<blocks, 1024, 0, s>>>(c, w, budget, n_sink, n_recent);
+    k_evict_list<<<blocks, 1024, 0, s>>>(c, w, budget);
+    k_evict_settle<<<heads, 1024, 0, s>>>(c, w, budget);
+    k_evict_number<<<blocks, 1024, 0, s>>>(c, w, to.in_place, budget);
+  } else {
+    k_evict_select<<<heads, 1024, 0, s>>>(c, w, to.in_place, budget, n_sink, n_recent);
+  }
   const int ch = c.d * (c.bf16 ? 2 : 4) / 16;
   const int64_t most = to.in_place ? std::min(budget, std::max(c.cap - budget, 1)) : budget;
   const unsigned blocks = (unsigned)std::min<int64_t>((most * ch + 255) / 256, 256);
-  k_evict_move<<<dim3(blocks, c.B * c.Hkv), 256, 0, s>>>(c, to, w, budget);
+  k_evict_move<<<dim3(blocks, heads), 256, 0, s>>>(c, to, w, budget);
 }
 
 }  // namespace sparsepr

@@ -562,6 +562,32 @@ def test_evict_orders(kind, n, other):
         c.dlen.copy_(ints(c.lens))
 
 
+@pytest.mark.parametrize("kind", ["equal", "ties", "close", "special", "descending", "ascending"])
+@pytest.mark.parametrize("n", [8193, 24577, 30011])
+@pytest.mark.parametrize("other", [0, 3])
+def test_evict_orders_of_large_caches(kind, n, other):
+    # scores that only the last bits or the slots tell apart, and entries of one
+    # launch that need nothing, little and much
+    c = Case("bf16", 64, b=3, hkv=2, g=1, cap=n, lens=(n, n // 2 + 1, n // 3), t=1)
+    rng = np.random.default_rng(n)
+    s = c.scores.numpy()
+    if kind == "equal":
+        s[:] = 0.5
+    elif kind == "ties":
+        s[:] = rng.integers(0, 3, s.shape)
+    elif kind == "close":  # neighbouring floats, each a few times
+        s[:] = (np.float32(1.0).view(np.int32) + rng.integers(0, 1500, s.shape)).astype(np.int32).view(np.float32)
+    elif kind == "special":
+        s[:] = rng.choice([0.0, -0.0, NAN, math.inf, -math.inf, 1e-45, -1e-45, 3e38, 1.0, -2.0], s.shape)
+    elif kind == "descending":
+        s[:] = -np.sort(-s, axis=2)
+    else:
+        s[:] = np.sort(s, axis=2)
+    for budget, sink, recent in ((n // 2, 0, 0), (n - 1, 5, 4000), (n // 3, 0, 1)):
+        run_evict(c, budget, sink, recent, other)
+        c.dlen.copy_(ints(c.lens))
+
+
 def test_evict_goes_by_positions_not_slots():
     # after evictions the slots are not in the order of time
     c = Case("bf16", 64, b=2, hkv=2, g=1, cap=500, lens=(500, 333), t=1)

@@ -421,9 +421,10 @@ typedef struct {
  * alone) and belongs to the call until its work has completed.
  * Errors (all four operators): INVALID_ARGUMENT for bad pointers, sizes and
  * ranges; UNSUPPORTED for d not in {64, 128}, rows of K, V, Q or the output
- * (base pointers and strides) not 16-byte aligned, n * heads / heads_kv or capacity above 2^28,
- * batch * heads_kv above 65535, a row stride of K or V above 2^24 elements, a
- * tree of more than 256 tokens. */
+ * (base pointers and strides) not 16-byte aligned, a row stride of K or V above
+ * 2^24 elements, capacity or n * heads / heads_kv (likewise n_rows) above 2^28,
+ * batch * heads * n of 2^31 or more, batch * heads_kv above 65535, a tree of
+ * more than 256 tokens. */
 sparsepr_status sparsepr_cache_attend_workspace_size(const sparsepr_cache* cache,
                                                      const sparsepr_tokens* tokens, size_t* bytes);
 sparsepr_status sparsepr_cache_attend(const sparsepr_cache* cache, const sparsepr_tokens* tokens,

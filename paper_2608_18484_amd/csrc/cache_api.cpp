@@ -16,6 +16,8 @@ using namespace sparsepr;
 namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 28;
+// Rows of all heads: a launch's blocks are counted in 31 bits.
+constexpr int64_t kMaxAllRows = int64_t(1) << 31;
 // The kernels address the 32 rows of a key tile by 32-bit byte offsets.
 constexpr int64_t kMaxRowStride = int64_t(1) << 24;
 
@@ -116,6 +118,7 @@ sparsepr_status tokens_ok(const sparsepr_tokens* t, CacheCall& x) {
   if (t->mask == SPARSEPR_TOKENS_TREE && t->n > kTreeMax) return unsupported("tokens: a tree has at most 256 tokens");
   x.G = t->heads / x.Hkv;
   if ((int64_t)t->n * x.G > kMaxRows) return unsupported("tokens: n * heads / heads_kv above 2^28");
+  if ((int64_t)t->n * x.G * x.Hkv * x.B >= kMaxAllRows) return unsupported("tokens: batch * heads * n above 2^31");
   x.T = t->n;
   x.mask = t->mask;
   x.qsb = t->stride_b;
@@ -171,12 +174,19 @@ sparsepr_status attend_geometry(const sparsepr_cache* cache, const sparsepr_toke
   return SPARSEPR_OK;
 }
 
-sparsepr_status rows_ok(CacheCall& x, const int32_t* rows, int32_t n_rows) {
+sparsepr_status row_count_ok(CacheCall& x, int32_t n_rows) {
   if (n_rows < 1) return bad("n_rows must be at least 1");
-  if (!rows && n_rows != x.T) return bad("n_rows must be the number of tokens when rows is NULL");
   if ((int64_t)n_rows * x.G > kMaxRows) return unsupported("n_rows * heads / heads_kv above 2^28");
-  x.rows = rows;
+  if ((int64_t)n_rows * x.G * x.Hkv * x.B >= kMaxAllRows) return unsupported("batch * heads * n_rows above 2^31");
   x.C = n_rows;
+  return SPARSEPR_OK;
+}
+
+sparsepr_status rows_ok(CacheCall& x, const int32_t* rows, int32_t n_rows) {
+  x.rows = rows;
+  const sparsepr_status st = row_count_ok(x, n_rows);
+  if (st != SPARSEPR_OK) return st;
+  if (!rows && n_rows != x.T) return bad("n_rows must be the number of tokens when rows is NULL");
   return SPARSEPR_OK;
 }
 
@@ -256,14 +266,12 @@ sparsepr_status sparsepr_cache_accumulate_workspace_size(const sparsepr_cache* c
                                                          int32_t n_rows, size_t* bytes) {
   return guarded([&]() -> sparsepr_status {
     if (!bytes) return bad("bytes must not be NULL");
-    if (n_rows < 1) return bad("n_rows must be at least 1");
     CacheCall x;
     sparsepr_status st = cache_ok(cache, x);
     if (st == SPARSEPR_OK) st = tokens_ok(tokens, x);
     if (st == SPARSEPR_OK) st = q_ok(x);
+    if (st == SPARSEPR_OK) st = row_count_ok(x, n_rows);
     if (st != SPARSEPR_OK) return st;
-    if ((int64_t)n_rows * x.G > kMaxRows) return unsupported("n_rows * heads / heads_kv above 2^28");
-    x.C = n_rows;
     *bytes = cache_accumulate_workspace(x);
     return set_error(SPARSEPR_OK, "");
   });

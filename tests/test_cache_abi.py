@@ -116,6 +116,7 @@ def test_attend_workspace_depends_on_geometry_alone():
     ({}, dict(mask=3), 1, "mask"),
     ({}, dict(n=257, mask=2), 2, "256"),
     ({}, dict(n=1 << 28), 2, "2^28"),
+    ({}, dict(n=1 << 27, stride_n=0, stride_h=0, stride_b=0, kv_stride_n=0), 2, "2^31"),
     ({}, dict(stride_n=-64), 1, "Q strides"),
     ({}, dict(stride_n=65), 2, "Q strides"),
     ({}, dict(kv_stride_n=-64), 1, "K/V strides"),
@@ -173,8 +174,11 @@ def test_lists_and_scores_refused():
         assert st == 1 and "n_rows" in msg
         st, msg = f(c, t, n_rows=4)  # all tokens are 5
         assert st == 1 and "n_rows" in msg
-        st, msg = f(c, t, rows=P, n_rows=1 << 28) if f is accumulate else (2, "2^28")
-        assert st == 2 and "2^28" in msg
+    st, msg = accumulate(c, t, rows=P, n_rows=1 << 28)
+    assert st == 2 and "2^28" in msg
+    for f in (append, accumulate):
+        st, msg = f(c, t, rows=P, n_rows=1 << 27)
+        assert st == 2 and "2^31" in msg
     st, msg = accumulate(cache(scores=None), t)
     assert st == 1 and "scores" in msg
     st, msg = evict(cache(scores=None))

@@ -72,12 +72,12 @@ __global__ __launch_bounds__(256) void k_cache_append_lengths(CacheCall c) {
 
 // Workspace of an eviction, per K/V head.
 struct EvictWork {
-  uint32_t* key;   // [cap_pad] the slots' keys
   int2* count;     // rows to move, rows kept
   int32_t* hole;   // [budget] freed slots below the budget
   int32_t* mover;  // [budget] kept slots behind it
   int32_t* stay;   // [budget] for another cache: the slot itself, ~i where it is the i-th freed
   // large caches
+  uint32_t* key;    // [cap_pad] the slots' keys
   int32_t* hist;    // [kBins] slots by the first digit of their key
   int32_t* newest;  // [blocks] largest position of a block's slots
   int2* part;       // [blocks] (freed, moving) slots of a block, then those before it
@@ -163,26 +163,27 @@ __device__ __forceinline__ int bin_of(const Hist& h, int x) {
   return v.x + v.y + v.z + v.w;
 }
 
+// Slots of the largest caches that one block a head takes: 6 turns of 4 slots a
+// thread, whose keys stay in registers.
+constexpr int kTurns = 6, kSmall = kTurns * 4096;
+
 // One block a K/V head: the budget-th largest key by digits of 11, 11 and 10
 // bits, then the freed and the moving slots numbered in their order.
 //
-// Every wave has a run of neighbouring slots and a lane four neighbours of
-// each 256, which it alone reads and writes: the first pass over the scores and
-// positions leaves the keys in the workspace, so that the later ones read four
-// bytes a slot by 16-byte loads from L2, several ahead, and the numbering
-// needs one exchange between the waves.  What bounds it is what one CU reads:
-// with loads of 4 bytes a pass over 75,606 slots took 10 us, keys kept in 80
-// registers a lane instead made 100 KB of code that every launch fetches anew.
+// Every wave has a run of neighbouring slots and a lane four neighbours of each
+// 256.  All of its scores and positions are read at once, so that memory is
+// waited for once, and the digits' passes go over registers; the numbering needs
+// one exchange between the waves.  What bounds it is one CU's issue of some 60
+// instructions a slot: 17,160 slots of 32 heads 25 us.  Keys that every pass read
+// again from L2 took 31; runs of neighbouring slots a thread, numbered by a scan
+// over the threads instead of ballots, 29: their loads and stores scatter.
 __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w, int in_place, int budget, int n_sink, int n_recent) {
   __shared__ Hist hist;
   __shared__ int wsum[3][16], sh_newest;
   const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = cache_length(c, bh / c.Hkv);
-  const float* score = c.scores + (size_t)bh * c.cap;
   const bool by_pos = n_sink > 0 || n_recent > 0;
-  const int32_t* pos = by_pos ? c.positions + (size_t)bh * c.cap : nullptr;
-  uint32_t* key = w.key + (size_t)bh * w.cap_pad;
   int32_t* hole = w.hole + (size_t)bh * budget;
   int32_t* mover = w.mover + (size_t)bh * budget;
   int32_t* stay = w.stay + (size_t)bh * budget;
@@ -192,93 +193,67 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
     if (tid == 0) w.count[bh] = make_int2(0, len);
     return;
   }
-  constexpr int AHEAD = 4;
   const int turns = (len + 4095) / 4096;  // of a wave, 256 slots each
   const int j0 = wv * turns * 256 + lane * 4;
-  int newest = INT_MIN;
-  if (n_recent > 0) {
+  uint32_t key[kTurns][4];
+  {
+    i32x4_u s[kTurns], p[kTurns];
+    const int32_t* score = (const int32_t*)c.scores + (size_t)bh * c.cap;
+    const int32_t* pos = by_pos ? c.positions + (size_t)bh * c.cap : nullptr;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int j = j0 + min(i, turns - 1) * 256;
+      s[i] = four(score, j, len);
+      p[i] = by_pos ? four(pos, j, len) : i32x4_u{};
+    }
     if (tid == 0) sh_newest = INT_MIN;
     __syncthreads();
-    for (int i = 0; i < turns; i += AHEAD) {
-      i32x4_u v[AHEAD];
+    int newest = INT_MIN;
+    if (n_recent > 0) {
 #pragma unroll
-      for (int x = 0; x < AHEAD; ++x) v[x] = four(pos, j0 + min(i + x, turns - 1) * 256, len);
+      for (int i = 0; i < kTurns; ++i) newest = max(newest, max(max(p[i].x, p[i].y), max(p[i].z, p[i].w)));
 #pragma unroll
-      for (int x = 0; x < AHEAD; ++x) newest = max(newest, max(max(v[x].x, v[x].y), max(v[x].z, v[x].w)));
+      for (int o = 32; o > 0; o >>= 1) newest = max(newest, __shfl_xor(newest, o));
+      if (lane == 0) atomicMax(&sh_newest, newest);
+      __syncthreads();
+      newest = sh_newest;
     }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) newest = max(newest, __shfl_xor(newest, o));
-    if (lane == 0) atomicMax(&sh_newest, newest);
-    __syncthreads();
-    newest = sh_newest;
+    for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        key[i][e] = i < turns && j0 + i * 256 + e < len ? evict_key(__int_as_float(s[i][e]), p[i][e], by_pos, n_sink, n_recent, newest) : 0;
   }
   // f(slot of the lane's first key, keys), in the order of the slots; every
   // lane of a wave takes part
   auto each = [&](auto&& f) {
-    for (int i = 0; i < turns; i += AHEAD) {
-      uint4 k[AHEAD];
 #pragma unroll
-      for (int x = 0; x < AHEAD; ++x) {
-        const int j = j0 + (i + x) * 256;
-        k[x] = i + x < turns && j < len ? *(const uint4*)(key + j) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int x = 0; x < AHEAD; ++x)
-        if (i + x < turns) f(j0 + (i + x) * 256, k[x]);
-    }
+    for (int i = 0; i < kTurns; ++i)
+      if (i < turns) f(j0 + i * 256, key[i]);
   };
   uint32_t prefix = 0, mask = 0;
   int need = budget, same = 0;  // keys still to take among those that match the prefix; those
   for (int shift = 21; shift >= 0; shift = shift > 10 ? 10 : shift > 0 ? 0 : -1) {
     hist_clear(hist);
     const int dmask = shift == 0 ? 1023 : 2047;
-    if (shift == 21) {
-      for (int i = 0; i < turns; i += AHEAD) {
-        i32x4_u s[AHEAD], p[AHEAD];
+    each([&](int, const uint32_t* k) {
+      bool on[4], any = false;
+      int digit[4];
 #pragma unroll
-        for (int x = 0; x < AHEAD; ++x) {
-          const int j = j0 + min(i + x, turns - 1) * 256;
-          s[x] = four((const int32_t*)score, j, len);
-          if (by_pos) p[x] = four(pos, j, len);
-        }
-#pragma unroll
-        for (int x = 0; x < AHEAD; ++x) {
-          if (i + x >= turns) continue;
-          const int j = j0 + (i + x) * 256;
-          uint32_t k[4];
-          bool on[4];
-          int digit[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            k[e] = evict_key(__int_as_float(s[x][e]), by_pos ? p[x][e] : 0, by_pos, n_sink, n_recent, newest);
-            if (j + e >= len) k[e] = 0;
-            on[e] = j + e < len;
-            digit[e] = (int)(k[e] >> 21);
-          }
-          hist_add(hist, on, digit, lane);
-          if (j < len) *(uint4*)(key + j) = make_uint4(k[0], k[1], k[2], k[3]);
-        }
+      for (int e = 0; e < 4; ++e) {
+        on[e] = k[e] != 0 && (k[e] & mask) == prefix;
+        digit[e] = (int)(k[e] >> shift) & dmask;
+        any |= on[e];
       }
-    } else {
-      each([&](int, uint4 k4) {
-        const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
-        bool on[4], any = false;
-        int digit[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          on[e] = k[e] != 0 && (k[e] & mask) == prefix;
-          digit[e] = (int)(k[e] >> shift) & dmask;
-          any |= on[e];
-        }
-        if (__ballot(any)) hist_add(hist, on, digit, lane);
-      });
-    }
+      if (__ballot(any)) hist_add(hist, on, digit, lane);
+    });
     __syncthreads();
     hist_find(hist, bin_of(hist, kBins - 1 - 2 * tid), bin_of(hist, kBins - 2 - 2 * tid), need);
     need = hist.need;
     same = hist.same;
     prefix |= (uint32_t)hist.digit << shift;
     mask |= (uint32_t)dmask << shift;
+    __syncthreads();
     if (same == need) break;  // all that match stay: the lower digits do not matter
   }
   // keys above `prefix` stay, and all that match it, or the first `need` of them
@@ -293,11 +268,10 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
   auto total = [&](const uint64_t* m) { return (int)(__popcll(m[0]) + __popcll(m[1]) + __popcll(m[2]) + __popcll(m[3])); };
   if (ties) {
     int n_eq = 0;
-    each([&](int, uint4 k) {
-      const uint64_t m[4] = {__ballot(k.x == prefix), __ballot(k.y == prefix), __ballot(k.z == prefix), __ballot(k.w == prefix)};
+    each([&](int, const uint32_t* k) {
+      const uint64_t m[4] = {__ballot(k[0] == prefix), __ballot(k[1] == prefix), __ballot(k[2] == prefix), __ballot(k[3] == prefix)};
       n_eq += total(m);
     });
-    __syncthreads();
     if (lane == 0) wsum[0][wv] = n_eq;
     __syncthreads();
     for (int x = 0; x < wv; ++x) eq0 += wsum[0][x];
@@ -305,15 +279,10 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
   // f(first slot, freed, moves, ballots of both) in the order of the slots
   auto number = [&](auto&& f) {
     int eq = eq0;
-    each([&](int j, uint4 k4) {
-      const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+    each([&](int j, const uint32_t* k) {
       bool keep[4], freed[4], moves[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) keep[e] = k[e] >= prefix;
-      // 256 slots of which all stay or all go where that is nothing new
-      const int first = __builtin_amdgcn_readfirstlane(j);
-      if (!ties && in_place && first + 256 <= budget && __ballot(keep[0] && keep[1] && keep[2] && keep[3]) == ~0ull) return;
-      if (!ties && first >= budget && !__ballot(keep[0] || keep[1] || keep[2] || keep[3])) return;
       if (ties) {
         uint64_t m[4];
 #pragma unroll
@@ -353,9 +322,9 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
     int rf = at_hole + ahead(bf), rm = at_move + ahead(bm);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
+      if (!in_place && j + e < budget) stay[j + e] = freed[e] ? ~rf : j + e;
       if (freed[e]) hole[rf++] = j + e;
       if (moves[e]) mover[rm++] = j + e;
-      if (!in_place && j + e < budget) stay[j + e] = freed[e] ? ~(rf - 1) : j + e;
     }
     at_hole += total(bf);
     at_move += total(bm);
@@ -645,10 +614,10 @@ __global__ __launch_bounds__(256) void k_evict_move(CacheCall c, EvictTo to, Evi
 }
 
 // Beyond 24,576 slots a head's slots are shared by several blocks, in five
-// launches: 75,600 slots of 16 heads 39 us with an append, one block a head 51;
-// 32,000 slots of 8 heads cut to 4,000 43 and 49; but 17,160 of 32 heads 63 and
-// 57, 9,000 of 8 heads 40 and 28.
-bool evict_large(const CacheCall& c) { return c.cap > 24576; }
+// launches: 75,600 slots of 16 heads 39 us with an append, by one block a head
+// (reading the keys again for every pass) 51; 25,000 slots of 8 heads cut to 4,000
+// take 35 us so, 24,000 by one block a head 36; 17,160 of 32 heads 63 and 49.
+bool evict_large(const CacheCall& c) { return c.cap > kSmall; }
 
 // The workspace's arrays in their order (ws null: their bytes alone).
 size_t evict_layout(const CacheCall& c, int budget, void* ws, EvictWork& w) {
@@ -660,12 +629,12 @@ size_t evict_layout(const CacheCall& c, int budget, void* ws, EvictWork& w) {
     p = (std::remove_reference_t<decltype(p)>)((char*)ws + at);
     at += (n * per_head * sizeof(*p) + 15) / 16 * 16;
   };
-  take(w.key, w.cap_pad);
   take(w.count, 1);
   take(w.hole, budget);
   take(w.mover, budget);
   take(w.stay, budget);
   if (!evict_large(c)) return at;
+  take(w.key, w.cap_pad);
   take(w.hist, kBins);
   take(w.newest, w.blocks);
   take(w.part, w.blocks);

@@ -25,8 +25,9 @@ constexpr int kKeys = 32;  // keys of a tile
 // entry has some steps, known on the device alone; a part is `per` consecutive
 // ones of an entry (the last part of an entry is shorter), and the parts are
 // numbered in the order of the entries.  All of this is called by whole waves;
-// up to 64 entries are read once (a lane each), which keeps one trip to memory
-// between the start of a block and its first keys.
+// up to 64 entries are read once (a lane each; a single one by all lanes, with
+// nothing to exchange), which keeps one trip to memory between the start of a
+// block and its first keys.
 __device__ __forceinline__ int parts_of(int steps, int per) {
   const uint32_t n = (uint32_t)steps / (uint32_t)per;
   return (int)(n + (n * (uint32_t)per != (uint32_t)steps));
@@ -42,7 +43,7 @@ struct Parts {
   int most;       // tokens of an entry at most
   F steps;        // of an Entry
   int lane;
-  Entry own;      // of entry `lane`
+  Entry own;      // of entry `lane`, or of the only one
   int own_steps;
   int per;        // steps of a part
 
@@ -57,18 +58,19 @@ struct Parts {
   // B - 1 more where they are ragged.  0: one part an entry.
   __device__ __forceinline__ Parts(const CacheCall& call, int parts, int most_tokens, int lane_, F f)
       : c(call), most(most_tokens), steps(f), lane(lane_), own{0, 0}, own_steps(0), per(0x7fffffff) {
-    if (lane < c.B) {
-      own = entry(lane);
+    if (lane < c.B || c.B == 1) {
+      own = entry(c.B == 1 ? 0 : lane);
       own_steps = steps(own);
     }
     if (parts == 0) return;
     // (K, V and the rows are in memory, so that their tiles' number fits 31 bits)
-    int total = 0;
-    for (int b0 = 0; b0 < c.B; b0 += 64) total += wave_sum_i(at(b0, c.B));
+    int total = c.B == 1 ? own_steps : 0;
+    for (int b0 = 0; b0 < c.B && c.B > 1; b0 += 64) total += wave_sum_i(at(b0, c.B));
     per = max(((uint32_t)total + (uint32_t)parts - 1) / (uint32_t)parts, 1u);
   }
   // parts of the first B entries
   __device__ __forceinline__ int count(int B) const {
+    if (c.B == 1) return B == 1 ? parts_of(own_steps, per) : 0;
     int used = 0;
     for (int b0 = 0; b0 < B; b0 += 64) used += wave_sum_i(parts_of(at(b0, B), per));
     return used;
@@ -79,6 +81,15 @@ struct Parts {
   };
   __device__ __forceinline__ Found find(int slot) const {
     Found p{-1, 0, 0, 0, {0, 0}};
+    if (c.B == 1) {
+      p.count = parts_of(own_steps, per);
+      if (slot >= p.count) return p;
+      p.b = 0;
+      p.first = (int)min((int64_t)slot * per, (int64_t)own_steps);
+      p.last = (int)min((int64_t)(slot + 1) * per, (int64_t)own_steps);
+      p.e = own;
+      return p;
+    }
     for (int b0 = 0; b0 < c.B; b0 += 64) {
       const int st = at(b0, c.B), n = parts_of(st, per);
       int upto = n;

@@ -409,7 +409,6 @@ def dense_attention(q, k, v, out=None, stream=None):
 def _tensor(name, t, shape, dtype, device, contiguous=True):
     """Raises ValueError unless t is a tensor of this shape, dtype and device,
     contiguous or with a contiguous last dimension."""
-    import torch
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
     if t.device != device:
@@ -454,7 +453,8 @@ class KVCache:
     device) and never synchronise; flags() does."""
 
     def __init__(self, k, v, lengths, scores=None, positions=None):
-        import torch
+        global torch
+        import torch  # once for the module: the calls below look it up as a global
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
             raise ValueError("k: expected a [B, H_kv, capacity, d] torch.Tensor")
         if k.dtype not in (torch.bfloat16, torch.float32):
@@ -485,7 +485,6 @@ class KVCache:
     def flags(self) -> list:
         """CACHE_FLAG_* raised on the device since the last call, per batch
         entry; clears them.  Waits for the device."""
-        import torch
         torch.cuda.synchronize(self.device)
         got = self._flags.tolist()
         self._flags.zero_()
@@ -498,7 +497,6 @@ class KVCache:
         """launch(stream handle), with the stream and the cache's device current
         where they are not, so that scratch memory and outputs made by the call
         belong to the stream that uses them."""
-        import torch
         if stream is None:
             handle = torch.cuda.current_stream(self.device).cuda_stream
             if self.device.index == torch.cuda.current_device():
@@ -512,7 +510,6 @@ class KVCache:
 
     def _scratch(self, size_fn, *args):
         """Scratch memory of one call from torch's allocator (None if it needs none)."""
-        import torch
         need = ctypes.c_size_t(0)
         _check(size_fn(self._desc, *args, ctypes.addressof(need)))
         if need.value == 0:
@@ -520,7 +517,6 @@ class KVCache:
         return torch.empty(need.value, dtype=torch.uint8, device=self.device), need.value
 
     def _q(self, q):
-        import torch
         c = self.desc
         if not isinstance(q, torch.Tensor) or q.dim() != 4:
             raise ValueError("q: expected a [B, H, n, d] torch.Tensor")
@@ -540,7 +536,6 @@ class KVCache:
 
     def _list(self, rows, counts, n):
         """Checks an accepted-rows list and the counts; the list's width."""
-        import torch
         b, width = self.desc.batch, n
         if rows is not None:
             if not isinstance(rows, torch.Tensor) or rows.dim() != 2 or rows.shape[1] < 1:
@@ -561,7 +556,6 @@ class KVCache:
         it they are a chain (causal) or all see each other.  counts [B] int32:
         tokens of each entry.  Returns (out, lse); rows behind counts keep what
         the given out and lse hold (zeros where they are made here)."""
-        import torch
         h, n = self._q(q)
         ks = self._new(k_new, v_new, n)
         b = self.desc.batch
@@ -601,7 +595,6 @@ class KVCache:
         see sparsepr_cache_append.  positions [B, n] int32: the tokens'
         positions (with a cache that keeps them).  The new lengths go to
         lengths_out [B] int32, or into the cache's own."""
-        import torch
         if not isinstance(k_new, torch.Tensor) or k_new.dim() != 4 or k_new.shape[2] < 1:
             raise ValueError("k_new: expected a [B, H_kv, n, d] torch.Tensor with n >= 1")
         c, n = self.desc, k_new.shape[2]
@@ -623,7 +616,6 @@ class KVCache:
         """Add the attention weights of the rows that were just appended (rows
         and counts as in append; q and lse as in attend) to the scores of the
         slots that they see; see sparsepr_cache_accumulate."""
-        import torch
         h, n = self._q(q)
         c = self.desc
         width = self._list(rows, counts, n)

@@ -151,6 +151,7 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
   constexpr int TE = kKeys * D;         // elements of a tile
   static_assert(NCP % RS == 0, "copies divide among the waves of a tile");
   __shared__ __attribute__((aligned(1024))) uint16_t kv[KS][2][2][TE];  // [tile][buffer][K, V]
+  __shared__ float2 ml[KS > 1 ? 4 : 1][64];
   __shared__ Tree tree;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -381,64 +382,72 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
     }
   }
 
-  // join the key tiles' waves of each set of rows
-  if (KS > 1) {
-    constexpr int NREG = 16 * NDB;
-    static_assert((KS - 1) * RS * (NREG + 2) * 64 * 4 <= (int)sizeof(kv), "parts fit the tiles' memory");
-    float* red = (float*)&kv[0][0][0][0];
-    __syncthreads();
-    if (ks > 0) {
-      float* dst = red + (((ks - 1) * RS + rs) * (NREG + 2)) * 64 + lane;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) dst[(db * 16 + e) * 64] = O[db][e];
-      dst[NREG * 64] = m_run;
-      dst[(NREG + 1) * 64] = l_tot;
-    }
-    __syncthreads();
-    if (ks > 0) return;
-    for (int x = 1; x < KS; ++x) {
-      const float* src = red + (((x - 1) * RS + rs) * (NREG + 2)) * 64 + lane;
-      const float mp = src[NREG * 64], lp = src[(NREG + 1) * 64];
-      const float m_new = fmaxf(m_run, mp);
-      const float fa = __builtin_amdgcn_exp2f(m_run - m_new), fb = __builtin_amdgcn_exp2f(mp - m_new);
-      m_run = m_new;
-      l_tot = l_tot * fa + lp * fb;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) O[db][e] = O[db][e] * fa + src[(db * 16 + e) * 64] * fb;
-    }
-  }
-  if (!valid) return;
-  if (w.parts > 1) {
-    const size_t at_row = ((size_t)w.slot * c.Hkv + hk) * ((size_t)c.T * c.G) + row;
-    float* dst = cut.o + at_row * D;
-    if (h == 0) cut.ml[at_row] = make_float2(m_run, l_tot);
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4)
-        *(float4*)(dst + db * 32 + (e >> 2) * 8 + h * 4) = make_float4(O[db][e], O[db][e + 1], O[db][e + 2], O[db][e + 3]);
-    return;
-  }
-  const float inv = 1.f / l_tot;
+  const size_t at_row = ((size_t)w.slot * c.Hkv + hk) * ((size_t)c.T * c.G) + row;
+  float* part = cut.o + at_row * D;
   uint16_t* dst = (uint16_t*)c.out + b * c.osb + hq * c.osh + tok * c.osn;
-#pragma unroll
-  for (int db = 0; db < NDB; ++db)
-#pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-      uint32_t o[2];
-#pragma unroll
-      for (int x = 0; x < 4; x += 2) {
-        const uint16_t lo = __builtin_bit_cast(uint16_t, (__bf16)(O[db][e + x] * inv));
-        const uint16_t hi = __builtin_bit_cast(uint16_t, (__bf16)(O[db][e + x + 1] * inv));
-        o[x >> 1] = (uint32_t)lo | ((uint32_t)hi << 16);
-      }
-      *(uint2*)(dst + db * 32 + (e >> 2) * 8 + h * 4) = make_uint2(o[0], o[1]);
+  // registers 4 r4 .. 4 r4 + 3 of the output: four neighbouring channels
+  auto store = [&](int r4, float4 o, float l) {
+    const int dv = (r4 >> 2) * 32 + (r4 & 3) * 8 + h * 4;
+    if (w.parts > 1) {
+      *(float4*)(part + dv) = o;
+      return;
     }
-  if (h == 0 && c.lse) c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok] = (m_run + log2f(l_tot)) * 0.6931471805599453f;
+    const float inv = 1.f / l, y[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+    uint32_t z[2];
+#pragma unroll
+    for (int x = 0; x < 4; x += 2)
+      z[x >> 1] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[x]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[x + 1]) << 16;
+    *(uint2*)(dst + dv) = make_uint2(z[0], z[1]);
+  };
+  constexpr int NR4 = 4 * NDB;
+  if constexpr (KS > 1) {
+    // join the waves of each set of rows: every wave leaves its part in the
+    // tiles' memory and joins a share of the registers
+    static_assert(4 * NR4 * 64 * 16 <= (int)sizeof(kv), "parts fit the tiles' memory");
+    float4* red = (float4*)&kv[0][0][0][0] + lane;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < NR4; ++r)
+      red[(wv * NR4 + r) * 64] = make_float4(O[r >> 2][(r & 3) * 4], O[r >> 2][(r & 3) * 4 + 1], O[r >> 2][(r & 3) * 4 + 2], O[r >> 2][(r & 3) * 4 + 3]);
+    ml[wv][lane] = make_float2(m_run, l_tot);
+    __syncthreads();
+    if (!valid) return;
+    float f[KS];
+    m_run = ml[rs][lane].x;
+#pragma unroll
+    for (int x = 1; x < KS; ++x) m_run = fmaxf(m_run, ml[x * RS + rs][lane].x);
+    l_tot = 0.f;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const float2 y = ml[x * RS + rs][lane];
+      f[x] = __builtin_amdgcn_exp2f(y.x - m_run);
+      l_tot += y.y * f[x];
+    }
+#pragma unroll
+    for (int r = 0; r < NR4 / KS; ++r) {
+      const int r4 = ks * (NR4 / KS) + r;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        const float4 y = red[((x * RS + rs) * NR4 + r4) * 64];
+        o.x += y.x * f[x];
+        o.y += y.y * f[x];
+        o.z += y.z * f[x];
+        o.w += y.w * f[x];
+      }
+      store(r4, o, l_tot);
+    }
+  } else {
+    if (!valid) return;
+#pragma unroll
+    for (int r = 0; r < NR4; ++r)
+      store(r, make_float4(O[r >> 2][(r & 3) * 4], O[r >> 2][(r & 3) * 4 + 1], O[r >> 2][(r & 3) * 4 + 2], O[r >> 2][(r & 3) * 4 + 3]), l_tot);
+  }
+  if (ks > 0 || h > 0) return;
+  if (w.parts > 1)
+    cut.ml[at_row] = make_float2(m_run, l_tot);
+  else if (c.lse)
+    c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok] = (m_run + log2f(l_tot)) * 0.6931471805599453f;
 }
 
 // The same for fp32 on v_mfma_f32_32x32x2_f32.  Both contractions may take
@@ -451,9 +460,10 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
 template <int D, int RS>
 __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(CacheCall c, Cut cut) {
   constexpr int KS = 4 / RS;
-  constexpr int NQ = D / 8, HQ = NQ / 2, NDB = D / 32, NREG = 16 * NDB;
+  constexpr int NQ = D / 8, HQ = NQ / 2, NDB = D / 32;
   typedef float fv __attribute__((ext_vector_type(NDB)));
-  __shared__ float red[KS > 1 ? (KS - 1) * RS : 1][NREG + 2][64];
+  __shared__ fv red[KS > 1 ? 4 : 1][16][64];
+  __shared__ float2 ml[KS > 1 ? 4 : 1][64];
   __shared__ Tree tree;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -585,42 +595,61 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(Cach
       }
     }
   }
-  if (KS > 1) {
-    if (ks > 0) {
-      float(*dst)[64] = red[(ks - 1) * RS + rs];
-#pragma unroll
-      for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) dst[db * 16 + e][lane] = O[db][e];
-      dst[NREG][lane] = m_run;
-      dst[NREG + 1][lane] = l_tot;
-    }
-    __syncthreads();
-    if (ks > 0) return;
-    for (int x = 1; x < KS; ++x) {
-      const float(*src)[64] = red[(x - 1) * RS + rs];
-      const float mp = src[NREG][lane], lp = src[NREG + 1][lane];
-      const float m_new = fmaxf(m_run, mp);
-      const float fa = __builtin_amdgcn_exp2f(m_run - m_new), fb = __builtin_amdgcn_exp2f(mp - m_new);
-      m_run = m_new;
-      l_tot = l_tot * fa + lp * fb;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) O[db][e] = O[db][e] * fa + src[db * 16 + e][lane] * fb;
-    }
-  }
-  if (!valid) return;
   const size_t at_row = ((size_t)w.slot * c.Hkv + hk) * ((size_t)c.T * c.G) + row;
   float* dst = w.parts > 1 ? cut.o + at_row * D : (float*)c.out + b * c.osb + hq * c.osh + tok * c.osn;
+  // register e of all blocks: NDB neighbouring channels
+  auto store = [&](int e, fv o, float l) {
+    if (w.parts == 1) {
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    fv o;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) o[db] = w.parts > 1 ? O[db][e] : O[db][e] / l_tot;
+      for (int db = 0; db < NDB; ++db) o[db] /= l;
+    }
     *(fv*)(dst + ((e >> 2) * 8 + 4 * h + (e & 3)) * NDB) = o;
+  };
+  if constexpr (KS > 1) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      fv o;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) o[db] = O[db][e];
+      red[wv][e][lane] = o;
+    }
+    ml[wv][lane] = make_float2(m_run, l_tot);
+    __syncthreads();
+    if (!valid) return;
+    float f[KS];
+    m_run = ml[rs][lane].x;
+#pragma unroll
+    for (int x = 1; x < KS; ++x) m_run = fmaxf(m_run, ml[x * RS + rs][lane].x);
+    l_tot = 0.f;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const float2 y = ml[x * RS + rs][lane];
+      f[x] = __builtin_amdgcn_exp2f(y.x - m_run);
+      l_tot += y.y * f[x];
+    }
+#pragma unroll
+    for (int r = 0; r < 16 / KS; ++r) {
+      const int e = ks * (16 / KS) + r;
+      fv o{};
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        const fv y = red[x * RS + rs][e][lane];
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) o[db] += y[db] * f[x];
+      }
+      store(e, o, l_tot);
+    }
+  } else {
+    if (!valid) return;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      fv o;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) o[db] = O[db][e];
+      store(e, o, l_tot);
+    }
   }
-  if (h > 0) return;
+  if (ks > 0 || h > 0) return;
   if (w.parts > 1)
     cut.ml[at_row] = make_float2(m_run, l_tot);
   else if (c.lse)

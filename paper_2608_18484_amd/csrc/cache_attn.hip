@@ -796,7 +796,7 @@ void attend(const CacheCall& c, const Cut& cut, hipStream_t s) {
     else
       k_cache_join<D, 0, alone.value><<<blocks, 256, 0, s>>>(c, cut);
   };
-  if (cut.parts <= 8)
+  if (cut.parts <= 16 * c.B)
     join(std::true_type{});
   else
     join(std::false_type{});

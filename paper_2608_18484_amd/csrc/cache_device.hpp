@@ -21,6 +21,11 @@ __device__ __forceinline__ void raise_flag(const CacheCall& c, int b, int flag) 
 
 constexpr int kKeys = 32;  // keys of a tile
 
+// A value that all lanes of the wave hold alike, told to the compiler: what
+// follows from it stays in scalar registers (sums over lanes look different in
+// every lane to it, and with them every loop bound and address).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // The work of a launch, cut into parts of equal length over all entries.  An
 // entry has some steps, known on the device alone; a part is `per` consecutive
 // ones of an entry (the last part of an entry is shorter), and the parts are
@@ -66,14 +71,15 @@ struct Parts {
     // (K, V and the rows are in memory, so that their tiles' number fits 31 bits)
     int total = c.B == 1 ? own_steps : 0;
     for (int b0 = 0; b0 < c.B && c.B > 1; b0 += 64) total += wave_sum_i(at(b0, c.B));
+    total = uniform(total);
     per = max(((uint32_t)total + (uint32_t)parts - 1) / (uint32_t)parts, 1u);
   }
   // parts of the first B entries
   __device__ __forceinline__ int count(int B) const {
-    if (c.B == 1) return B == 1 ? parts_of(own_steps, per) : 0;
+    if (c.B == 1) return B == 1 ? parts_of(uniform(own_steps), per) : 0;
     int used = 0;
     for (int b0 = 0; b0 < B; b0 += 64) used += wave_sum_i(parts_of(at(b0, B), per));
-    return used;
+    return uniform(used);
   }
   struct Found {
     int b, first, last, count;  // entry (-1: none), its steps [first, last), its parts
@@ -82,12 +88,13 @@ struct Parts {
   __device__ __forceinline__ Found find(int slot) const {
     Found p{-1, 0, 0, 0, {0, 0}};
     if (c.B == 1) {
-      p.count = parts_of(own_steps, per);
+      const int all = uniform(own_steps);
+      p.count = parts_of(all, per);
       if (slot >= p.count) return p;
       p.b = 0;
-      p.first = (int)min((int64_t)slot * per, (int64_t)own_steps);
-      p.last = (int)min((int64_t)(slot + 1) * per, (int64_t)own_steps);
-      p.e = own;
+      p.first = (int)min((int64_t)slot * per, (int64_t)all);
+      p.last = (int)min((int64_t)(slot + 1) * per, (int64_t)all);
+      p.e = Entry{uniform(own.len), uniform(own.n)};
       return p;
     }
     for (int b0 = 0; b0 < c.B; b0 += 64) {
@@ -100,16 +107,16 @@ struct Parts {
       }
       const uint64_t over = __ballot(upto > slot);
       if (over) {
-        const int l = __builtin_ctzll(over);
-        const int before = slot - __shfl(upto - n, l), all = __shfl(st, l);
+        const int l = (int)__builtin_ctzll(over);
+        const int before = slot - __builtin_amdgcn_readlane(upto - n, l), all = __builtin_amdgcn_readlane(st, l);
         p.b = b0 + l;
-        p.count = __shfl(n, l);
+        p.count = __builtin_amdgcn_readlane(n, l);
         p.first = (int)min((int64_t)before * per, (int64_t)all);
         p.last = (int)min((int64_t)(before + 1) * per, (int64_t)all);
-        p.e = b0 == 0 ? Entry{__shfl(own.len, l), __shfl(own.n, l)} : entry(p.b);
+        p.e = b0 == 0 ? Entry{__builtin_amdgcn_readlane(own.len, l), __builtin_amdgcn_readlane(own.n, l)} : entry(p.b);
         return p;
       }
-      slot -= __shfl(upto, 63);
+      slot -= __builtin_amdgcn_readlane(upto, 63);
     }
     return p;
   }

@@ -40,7 +40,7 @@ __device__ __forceinline__ int weigh_parts(const CacheCall& c, const WeighCut& w
   int used = 0;
   for (int b0 = 0; b0 < c.B; b0 += 64)
     used += wave_sum_i(b0 + lane < c.B ? (cache_length(c, b0 + lane) + keys - 1) / keys : 0);
-  used *= c.Hkv;
+  used = uniform(used) * c.Hkv;
   int best = 1;
   for (int p = 2; p <= w.parts_max; ++p) {
     const int64_t now = (used * (int64_t)p + w.room - 1) / w.room, was = (used * (int64_t)best + w.room - 1) / w.room;

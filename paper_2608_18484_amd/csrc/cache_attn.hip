@@ -330,7 +330,8 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
     // the waves of a tile share its copies; the scores of the next tile are
     // formed next to the exponentials of this one, the copies of K run two
     // tiles ahead and those of V one, with one barrier a step
-    const bool active = w.row0 + rs * 32 < w.rows;
+    // (with one tile a step every wave runs every step, also one without rows: a
+    // branch around the products would copy the scores)
     int i = t_first + ks;  // this wave's tile
     f32x16 S0, S1;
     float mt = 0.f;
@@ -340,7 +341,7 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
       __syncthreads();
       if (i + 2 * KS < t_last) issue(i + 2 * KS, 0, b);
       if (i + KS < t_last) issue(i + KS, 1, 1 - b);
-      if (active && i < t_last) {
+      if (KS == 1 || i < t_last) {
         finish(Sc, mt, b, [&] { scores(Sn, 1 - b); });
         if (i + KS < t_last) mt = mask_max(Sn, i + KS);
       }
@@ -350,7 +351,7 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
     if (i + KS < t_last) issue(i + KS, 0, 1);
     wait_copies<0>();
     __syncthreads();
-    if (active && i < t_last) {
+    if (KS == 1 || i < t_last) {
       scores(S0, 0);
       mt = mask_max(S0, i);
     }

@@ -35,8 +35,7 @@ struct Cut {
   int row_tiles;    // tiles of 32 RS rows of an entry and K/V head
   int ks;           // key tiles of a step
   int split;        // 0: one part per entry
-  int parts;        // split: parts of all entries aimed at (of each head and row tile)
-  int slots;        // parts of all entries at most
+  int slots;        // parts of all entries at most (of each head and row tile)
   float* o;         // [slots][Hkv][T G][D] parts' outputs, relative to their maxima
   float2* ml;       // [slots][Hkv][T G] maxima (base 2) and sums
 };
@@ -107,7 +106,7 @@ struct Where {
 // use, the row tiles of a part and head next to each other, which read the
 // same keys.
 __device__ __forceinline__ bool locate(const CacheCall& c, const Cut& cut, int tile_rows, int lane, Where& w) {
-  const auto all = cut_parts(c, cut.split ? cut.parts : 0, c.T, lane, steps_of(cut));
+  const auto all = cut_parts(c, cut.split ? cut.slots : 0, c.T, lane, steps_of(cut));
   const uint32_t used = (uint32_t)(all.count(c.B) * c.Hkv * cut.row_tiles), eighth = (used + 7) / 8;
   const uint32_t at = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
   if ((blockIdx.x >> 3) >= eighth || at >= used) return false;
@@ -659,7 +658,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(Cach
 
 // Join the parts of the rows whose keys were split.  D / 4 lanes hold a row; a
 // block has 1,024 / D such groups, one a row (ALONE) or all on one row's parts
-// in turn: the latter where rows have many parts.
+// in turn.
 template <int D, int BF16, bool ALONE>
 __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
   constexpr int L = D / 4, NG = 256 / L;
@@ -669,7 +668,7 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
   const int R = c.T * c.G, tiles = ALONE ? (R + NG - 1) / NG : R;
   const int bh = blockIdx.x / tiles, row = ALONE ? blockIdx.x % tiles * NG + g : blockIdx.x % tiles;
   const int b = bh / c.Hkv, hk = bh % c.Hkv;
-  const auto all = cut_parts(c, cut.parts, c.T, lane, steps_of(cut));
+  const auto all = cut_parts(c, cut.slots, c.T, lane, steps_of(cut));
   // this entry's parts follow those of the entries before it
   const int first = all.count(b);
   const Entry e = c.B == 1 ? all.own : b < 64 ? Entry{__shfl(all.own.len, b), __shfl(all.own.n, b)} : all.entry(b);
@@ -730,9 +729,11 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
 // Sets of 32 rows of a block.  One where that holds all rows: four waves then
 // stream four key tiles, which a step waits for alone.  Else four, or two where
 // an odd number of 64-row tiles would leave half a 128-row tile empty (189 rows
-// over two caches of 75,600 slots 178 us, with four sets 202; 576 rows 202 and
-// 213) and the rows are few: many rows read the keys from L2 once more for
-// every tile (4,680 rows over 18,720 keys 431 us, with two sets 492).
+// over two caches of 75,600 slots 64 us, with four sets 69; 576 rows 67.1 and
+// 68.1) and the rows are few: many rows read the keys from L2 once more for
+// every tile (4,680 rows over 18,720 keys 430 us, with two sets 459).  One set
+// for fp32's few rows: 3 over 84,480 slots 598 us, with two 1,114; for bf16's it
+// is 237 and 238.
 int row_sets(const CacheCall& c) {
   const int64_t rows = (int64_t)c.T * c.G;
   if (rows <= 32) return 1;
@@ -740,33 +741,38 @@ int row_sets(const CacheCall& c) {
 }
 
 // Parts.  A CU holds one block of the 128 KB of tiles of 32-row blocks at
-// d = 128 (or of fp32's registers) and two of the others; at d = 64 one such
-// block a CU streams as fast (45.9 us for two caches of 60,000 slots, with two
-// 47.6).  The parts of an entry end together when a launch fills the chip a
-// whole number of times, so that `parts`, of which ragged entries make up to
-// B - 1 more, is the most that r rounds hold; more rounds than one where a part
-// is then shorter by a twelfth (a frame's 296 blocks: one part each 566 us, 3
-// parts in two rounds 450, 5 in three 431; 24 blocks: 21 parts 178, 42 in two
-// rounds 187).  Up to 512 keys one part is done before a second kernel would
-// have joined several (one token over 256 slots 12.7 us, in parts 15.8; 512:
-// 15.0 and 16.0; 1,021: 19.2 and 16.0).
+// d = 128 (or of fp32's registers) and two of the others (d = 64, two caches of
+// 20,000 slots: 22.5 us with two, 24.5 with one; fp32 over four of 84,480 267 and
+// 345).  The parts of an entry end together when a launch fills the chip a whole
+// number of times, so that there are at most as many as r rounds hold.  More
+// rounds than one where a part is then shorter by a twelfth: a round begins with
+// some 5 us that read nothing (a frame's 296 blocks: one part each 513 us, 3 parts
+// in two rounds 432, 5 in three 430; 24 blocks: 21 parts 156, 42 in two rounds
+// 168).  fp32's parts take so long that a 25th will do (24 blocks: 10 parts
+// 1,243 us, 21 in two rounds 1,121).
+//
+// Few keys are one part, done before a second kernel would have joined several:
+// one token over 700 slots 14.1 us, in parts 15.4, over 1,021 17.1 and 15.4; 189
+// rows of 16 heads over 700 17.5 and 22.5, over 1,021 20.9 and 24.8; fp32 over
+// 100 slots 16.2 and 15.9, over 300 21.1 and 15.4.
 Cut make_cut(const CacheCall& c) {
   Cut cut{};
   const int rs = row_sets(c);
   const int64_t rows = (int64_t)c.T * c.G;
   cut.ks = 4 / rs;
   cut.row_tiles = (int)((rows + 32 * rs - 1) / (32 * rs));
+  cut.slots = c.B;
+  if ((int64_t)c.cap + c.T <= (c.bf16 ? 768 : 128)) return cut;
   const int64_t units = (int64_t)c.Hkv * cut.row_tiles;  // blocks of a part
-  const int64_t room = rs == 1 || (!c.bf16 && c.d == 128) ? 256 : 512;
+  const int64_t room = c.d == 128 && (rs == 1 || !c.bf16) ? 256 : 512;
   double best = 1e30;
-  for (int r = 1; r <= 4 && (int64_t)c.cap + c.T > 512; ++r) {
-    const int64_t parts = r * room / units - (c.B - 1);
-    if (parts <= c.B || r / (double)parts >= best * 0.92) continue;
+  for (int r = 1; r <= 4; ++r) {
+    const int64_t parts = r * room / units;
+    if (parts <= c.B || r / (double)parts >= best * (c.bf16 ? 0.92 : 0.96)) continue;
     best = r / (double)parts;
-    cut.parts = (int)parts;
+    cut.slots = (int)parts;
+    cut.split = 1;
   }
-  cut.split = cut.parts > 0;
-  cut.slots = c.B + (cut.split ? cut.parts - 1 : 0);
   return cut;
 }
 
@@ -797,7 +803,12 @@ void attend(const CacheCall& c, const Cut& cut, hipStream_t s) {
     else
       k_cache_join<D, 0, alone.value><<<blocks, 256, 0, s>>>(c, cut);
   };
-  if (cut.parts <= 16 * c.B)
+  // Many rows are joined a group of lanes each: 3,024 rows of 21 parts 154.9 us
+  // in all, a block each 158.0; 37,440 rows of 5 430 and 460.  Few of them leave
+  // the chip empty then (2,016 rows 29.2 and 28.4), and a row of many parts has
+  // one group wait for all of them (64 entries, of which one has 60,000 slots: 59
+  // and 27).
+  if (heads * R > 2560 && cut.slots <= 32)
     join(std::true_type{});
   else
     join(std::false_type{});

@@ -59,8 +59,8 @@ struct Parts {
     return b0 + lane < B ? steps(entry(b0 + lane)) : 0;
   }
 
-  // `parts` > 0: the length at which all entries make that many parts, and up to
-  // B - 1 more where they are ragged.  0: one part an entry.
+  // `parts` >= B: about the least length at which all entries together make at
+  // most that many parts.  0: one part an entry.
   __device__ __forceinline__ Parts(const CacheCall& call, int parts, int most_tokens, int lane_, F f)
       : c(call), most(most_tokens), steps(f), lane(lane_), own{0, 0}, own_steps(0), per(0x7fffffff) {
     if (lane < c.B || c.B == 1) {
@@ -73,6 +73,18 @@ struct Parts {
     for (int b0 = 0; b0 < c.B && c.B > 1; b0 += 64) total += wave_sum_i(at(b0, c.B));
     total = uniform(total);
     per = max(((uint32_t)total + (uint32_t)parts - 1) / (uint32_t)parts, 1u);
+    if (c.B == 1) return;
+    // every entry but one may round up: at total / (parts - (B - 1)) they fit.
+    // Few entries leave lanes to try lengths between the two, all at once
+    const uint32_t sure = (uint32_t)(parts - (c.B - 1)), lo = (uint32_t)per;
+    per = max(((uint32_t)total + sure - 1) / sure, 1u);
+    if (c.B > 32) return;
+    const int bits = 32 - __builtin_clz(c.B - 1), e = lane & ((1 << bits) - 1);  // 2^bits lanes a length
+    const int st = __shfl(own_steps, e);
+    const uint32_t mine = lo + (((uint32_t)per - lo) * (uint32_t)((lane >> bits) + 1) >> (6 - bits));
+    int made = e < c.B ? parts_of(st, (int)mine) : 0;
+    for (int o = 0; o < bits; ++o) made += __shfl_xor(made, 1 << o);
+    per = __builtin_amdgcn_readlane((int)mine, (int)__builtin_ctzll(__ballot(made <= parts)));
   }
   // parts of the first B entries
   __device__ __forceinline__ int count(int B) const {

@@ -27,7 +27,7 @@ struct WeighCut {
   int parts_max;   // row parts at most; 1: sums go straight to the scores
   int room;        // blocks that the chip holds
   int tiles_max;   // row tiles of an entry and K/V head at most
-  int parts;       // few rows: parts of all entries aimed at (of each head)
+  int parts;       // few rows: parts of all entries at most (of each head)
   char* rows;      // [B Hkv][tiles_max] row tiles as they go to LDS
   float* zv;       // [B Hkv][tiles_max][2][32] the rows' lse (base 2), and the slots they see
   int2* span;      // [B Hkv][tiles_max] the fewest and the most slots that a row of the tile sees
@@ -425,8 +425,8 @@ size_t cache_accumulate_workspace(const CacheCall& c) {
 void launch_cache_accumulate(const CacheCall& c, void* ws, hipStream_t s) {
   WeighCut w = weigh_cut(c);
   if (few_rows(c)) {
-    w.parts = std::max(kRoom / c.Hkv - (c.B - 1), c.B);
-    const dim3 grid((unsigned)(w.parts + c.B - 1) * (unsigned)c.Hkv);
+    w.parts = std::max(kRoom / c.Hkv, c.B);
+    const dim3 grid((unsigned)w.parts * (unsigned)c.Hkv);
     if (c.bf16)
       c.d == 64 ? k_cache_weigh_few<64, uint16_t><<<grid, 256, 0, s>>>(c, w) : k_cache_weigh_few<128, uint16_t><<<grid, 256, 0, s>>>(c, w);
     else

@@ -449,6 +449,20 @@ __global__ __launch_bounds__(1024) void k_evict_list(CacheCall c, EvictWork w, i
     if (j + e < len && open && (int)(k[e] >> 21) == digit) w.cand[(size_t)bh * w.cap_pad + put++] = make_uint2(k[e], (uint32_t)(j + e));
 }
 
+// One more of every lane's keys that is `on` to place `at` of copies; where the
+// wave's agree (slots that nothing has weighed yet are listed by the thousand),
+// one addition.
+__device__ __forceinline__ void count_at(Hist& h, bool on, int at, int copy, int lane) {
+  const uint64_t all = __ballot(on);
+  if (!all) return;
+  const int first = __builtin_amdgcn_readlane(at, (int)__builtin_ctzll(all));
+  if (__ballot(on && at != first) == 0) {
+    if (lane == 0) atomicAdd(&h.bin[first][0], (int)__popcll(all));
+  } else if (on) {
+    atomicAdd(&h.bin[at][copy], 1);
+  }
+}
+
 // One block a head: which of the listed slots stay (by the key's other digits,
 // of equal keys the lowest slots), and the freed and moving slots before each
 // block.  The list's order does not matter.
@@ -469,19 +483,33 @@ __global__ __launch_bounds__(1024) void k_evict_settle(CacheCall c, EvictWork w,
   // two more digits of the key, then three of the slot: those that a list is
   // matched by so far
   uint32_t slot_at = 0, slot_mask = 0;
+  // f(there is one, key and slot) of the list, whole waves at a time, eight loads
+  // ahead of their use
+  auto each = [&](auto&& f) {
+    for (int i0 = 0; i0 < n; i0 += 8192) {
+      uint2 x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = cand[min(i0 + u * 1024 + tid, n - 1)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) f(i0 + u * 1024 + tid < n, x[u]);
+    }
+  };
   for (int pass = 0; pass < 5 && same > need; ++pass) {
     const bool by_slot = pass >= 2;
     const int shift = pass == 0 ? 10 : pass == 1 ? 0 : pass == 2 ? 18 : pass == 3 ? 7 : 0;
     const uint32_t dmask = pass == 1 ? 1023u : pass == 4 ? 127u : 2047u;
+    if (pass == 2 && c.cap <= 1 << 18) {  // (every slot's first digit is 0)
+      slot_mask = dmask << shift;
+      continue;
+    }
     __syncthreads();
     hist_clear(hist);
-    for (int i = tid; i < n; i += 1024) {
-      const uint2 x = cand[i];
-      if ((x.x & mask) != least || (x.y & slot_mask) != slot_at) continue;
+    each([&](bool on, uint2 x) {
+      on &= (x.x & mask) == least && (x.y & slot_mask) == slot_at;
       // slots count from the lowest: their digits are turned round
       const uint32_t d = by_slot ? dmask - ((x.y >> shift) & dmask) : (x.x >> shift) & dmask;
-      atomicAdd(&hist.bin[d][lane & (kCopies - 1)], 1);
-    }
+      count_at(hist, on, (int)d, lane & (kCopies - 1), lane);
+    });
     __syncthreads();
     hist_find(hist, bin_of(hist, kBins - 1 - 2 * tid), bin_of(hist, kBins - 2 - 2 * tid), need);
     need = hist.need;
@@ -505,20 +533,18 @@ __global__ __launch_bounds__(1024) void k_evict_settle(CacheCall c, EvictWork w,
     const int x = x0 + tid;
     int2 own = make_int2(0, 0);
     if (x < blocks) own = part[x];
-    hist.bin[tid][0] = 0;
-    hist.bin[tid][1] = 0;
+    hist.bin[tid * 2][0] = 0;
+    hist.bin[tid * 2 + 1][0] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += 1024) {
-      const uint2 v = cand[i];
+    each([&](bool on, uint2 v) {
       const uint32_t k = v.x & mask;
       const int s = (int)v.y, at = s / kSlots - x0;
       const bool keep = k > least || (k == least && s <= last);
-      if (at < 0 || at >= 1024) continue;
-      if (keep && s >= budget) atomicAdd(&hist.bin[at][1], 1);
-      if (!keep && s < budget) atomicAdd(&hist.bin[at][0], 1);
-    }
+      on &= at >= 0 && at < 1024 && keep == (s >= budget);
+      count_at(hist, on, at * 2 + (s >= budget), 0, lane);
+    });
     __syncthreads();
-    const int f = own.x + hist.bin[tid][0], m = own.y + hist.bin[tid][1];
+    const int f = own.x + hist.bin[tid * 2][0], m = own.y + hist.bin[tid * 2 + 1][0];
     int uf = f, um = m;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {

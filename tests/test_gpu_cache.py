@@ -749,3 +749,120 @@ def test_outputs_made_by_the_call_are_zero_behind_counts():
     out, lse = c.cache.attend(c.dq, c.dkn, c.dvn, counts=ints([5, 2]))
     assert (out[1, :, 2:] == 0).all() and (lse[1, :, 2:] == 0).all()
     assert out.shape == c.dq.shape and lse.shape == (2, 2, 5)
+
+
+# ---- many entries, long strides, graphs side by side --------------------------
+
+@pytest.mark.parametrize("dtype,b,hkv,g,t", [("bf16", 2, 1, 3, 1), ("bf16", 5, 2, 2, 9),
+                                             ("bf16", 33, 1, 2, 1), ("bf16", 70, 1, 1, 3),
+                                             ("bf16", 70, 1, 3, 45), ("f32", 7, 1, 2, 1),
+                                             ("f32", 70, 1, 1, 2)])
+def test_parts_of_many_entries(dtype, b, hkv, g, t):
+    # parts of very uneven entries; more entries than a wave has lanes
+    lens = [int(x) for x in np.random.default_rng(b).integers(0, 120, b)]
+    lens[b // 2] = 2900
+    lens[-1] = 1333
+    lens[0] = 0
+    run_attend(Case(dtype, 64, b=b, hkv=hkv, g=g, cap=2900, lens=lens, t=t, seed=b))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("t", [3, 40])
+def test_accumulate_of_many_entries(dtype, t):
+    b = 70
+    lens = [int(x) for x in np.random.default_rng(t).integers(0, 90, b)]
+    lens[67], lens[3] = 600, 0
+    rows = np.random.default_rng(5).integers(0, t, (b, t))
+    counts = [min(n, t) for n in lens]
+    run_accumulate(Case(dtype, 64, b=b, hkv=1, g=1, cap=600, lens=lens, t=t), rows=rows, counts=counts)
+
+
+def test_append_and_evict_of_many_entries():
+    b = 70
+    lens = [int(x) for x in np.random.default_rng(8).integers(0, 60, b)]
+    c = Case("bf16", 64, b=b, hkv=2, g=1, cap=64, lens=lens, t=5)
+    rows, tpos = np.tile(np.arange(5), (b, 1)), np.tile(1000 + np.arange(5), (b, 1))
+    k, v, sc, pos, new, flags = append_ref(c, rows, [5] * b, tpos)
+    c.cache.append(c.dkn, c.dvn, positions=ints(tpos))
+    torch.cuda.synchronize()
+    assert c.dlen.tolist() == new and c.cache.flags() == flags
+    assert same(c.dk, k) and same(c.dv, v)
+    assert torch.equal(c.dscores.cpu(), sc) and torch.equal(c.dpos.cpu(), pos)
+    run_evict(Case("bf16", 64, b=b, hkv=2, g=1, cap=64, lens=lens, t=1), 20, 2, 5)
+    run_evict(Case("bf16", 64, b=b, hkv=2, g=1, cap=64, lens=lens, t=1), 20, 2, 5, other=1)
+
+
+def far_apart(x, stride):
+    """x [B, H, N, d] on the device with rows `stride` elements apart."""
+    b, h, n, d = x.shape
+    assert b == h == 1
+    room = torch.empty((n - 1) * stride + d, dtype=x.dtype, device="cuda")
+    view = room.as_strided((1, 1, n, d), (room.numel(), room.numel(), stride, 1))
+    view.copy_(x)
+    return view
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_past_32_bits(dtype):
+    # rows 2^24 elements apart: the cache's slots and the new tokens' lie far behind 2^32 bytes
+    far = 1 << 24
+    c = Case(dtype, 64, b=1, hkv=1, g=2, cap=150, lens=(140,), t=5, fill=0.5)
+    c.dk, c.dv, c.dkn, c.dvn = (far_apart(x, far) for x in (c.k, c.v, c.kn, c.vn))
+    c.cache = S().KVCache(c.dk, c.dv, c.dlen, scores=c.dscores, positions=c.dpos)
+    assert 149 * far * c.dk.element_size() > 2 ** 32
+    run_attend(c)
+    run_accumulate(c)
+    c.scores = c.dscores.cpu()
+    rows, tpos = np.arange(5)[None], np.arange(500, 505)[None]
+    k, v, sc, pos, lens, flags = append_ref(c, rows, [5], tpos)
+    c.cache.append(c.dkn, c.dvn, positions=ints(tpos))
+    torch.cuda.synchronize()
+    assert c.dlen.tolist() == lens and flags == [0]
+    assert same(c.dk, k) and same(c.dv, v)
+    c.k, c.v, c.scores, c.pos, c.lens = k, v, sc, pos, lens
+    run_evict(c, 90, 4, 20)
+
+
+@pytest.mark.parametrize("t", [134, 250])
+def test_frame_of_far_apart_rows(t):
+    # many rows: the shared tiles of both attention and accumulation
+    far = 1 << 24
+    c = Case("bf16", 64, b=1, hkv=1, g=1, cap=140, lens=(140,), t=t, fill=0.5)
+    c.dk, c.dv = far_apart(c.k, far), far_apart(c.v, far)
+    c.cache = S().KVCache(c.dk, c.dv, c.dlen, scores=c.dscores, positions=c.dpos)
+    run_attend(c)
+    run_accumulate(c)
+
+
+def test_counts_are_clamped():
+    c = Case("bf16", 64, b=3, hkv=1, g=2, cap=40, lens=(40, 9, 20), t=5)
+    out, lse = c.cache.attend(c.dq, c.dkn, c.dvn)
+    o2, z2 = torch.full_like(out, 7.0), torch.full_like(lse, -5.0)
+    c.cache.attend(c.dq, c.dkn, c.dvn, counts=ints([99, 5, -4]), out=o2, lse=z2)
+    assert torch.equal(out[:2], o2[:2]) and torch.equal(lse[:2], z2[:2])
+    assert (o2[2] == 7.0).all() and (z2[2] == -5.0).all()
+
+
+def test_one_cache_on_two_streams_and_two_graphs():
+    # calls on one cache at the same time, each with a workspace of its own; graphs
+    # of two caches replayed in turn
+    cs = [Case("bf16", 128, b=2, hkv=2, g=3, cap=3000, lens=(3000, 700), t=9, seed=i) for i in range(2)]
+    want = [c.cache.attend(c.dq, c.dkn, c.dvn) for c in cs]
+    ss = [torch.cuda.Stream() for _ in cs]
+    torch.cuda.synchronize()
+    got = [cs[0].cache.attend(c.dq, cs[0].dkn, cs[0].dvn, stream=s)
+           for _ in range(5) for c, s in zip((cs[0], cs[0]), ss)]
+    torch.cuda.synchronize()
+    for o, z in got:
+        assert torch.equal(o, want[0][0]) and torch.equal(z, want[0][1])
+    graphs, outs = [], []
+    for c in cs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(c.cache.attend(c.dq, c.dkn, c.dvn))
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 0, 1):
+        outs[i][0].zero_()
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i][0], want[i][0]) and torch.equal(outs[i][1], want[i][1])

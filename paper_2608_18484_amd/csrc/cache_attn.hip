@@ -671,7 +671,7 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
   const auto all = cut_parts(c, cut.slots, c.T, lane, steps_of(cut));
   // this entry's parts follow those of the entries before it
   const int first = all.count(b);
-  const Entry e = c.B == 1 ? all.own : b < 64 ? Entry{__shfl(all.own.len, b), __shfl(all.own.n, b)} : all.entry(b);
+  const Entry e = c.B == 1 ? all.own : b < 64 ? Entry{__builtin_amdgcn_readlane(all.own.len, b), __builtin_amdgcn_readlane(all.own.n, b)} : all.entry(b);
   const int ntok = e.n, count = parts_of(all.steps(e), all.per);
   // (one part wrote its rows itself)
   if (count < 2 || row >= ntok * c.G || first + count > cut.slots) return;

@@ -26,6 +26,19 @@ constexpr int kKeys = 32;  // keys of a tile
 // every lane to it, and with them every loop bound and address).
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// Sum of this lane's value and those of the lanes before it, by all lanes of the
+// wave: within rows of 16 lanes, then over the rows, by moves between lanes that
+// take a few cycles each where an exchange through LDS takes a hundred.
+__device__ __forceinline__ int wave_upto(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4 and
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);  // 8 lanes before
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row 0's sum to row 1, 2's to 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // both rows' sum to 2 and 3
+  return x;
+}
+
 // The work of a launch, cut into parts of equal length over all entries.  An
 // entry has some steps, known on the device alone; a part is `per` consecutive
 // ones of an entry (the last part of an entry is shorter), and the parts are
@@ -59,6 +72,8 @@ struct Parts {
     return b0 + lane < B ? steps(entry(b0 + lane)) : 0;
   }
 
+  __device__ __forceinline__ static int sum(int x) { return __builtin_amdgcn_readlane(wave_upto(x), 63); }
+
   // `parts` >= B: about the least length at which all entries together make at
   // most that many parts.  0: one part an entry.
   __device__ __forceinline__ Parts(const CacheCall& call, int parts, int most_tokens, int lane_, F f)
@@ -69,9 +84,8 @@ struct Parts {
     }
     if (parts == 0) return;
     // (K, V and the rows are in memory, so that their tiles' number fits 31 bits)
-    int total = c.B == 1 ? own_steps : 0;
-    for (int b0 = 0; b0 < c.B && c.B > 1; b0 += 64) total += wave_sum_i(at(b0, c.B));
-    total = uniform(total);
+    int total = 0;
+    for (int b0 = 0; b0 < c.B; b0 += 64) total += sum(at(b0, c.B));
     per = max(((uint32_t)total + (uint32_t)parts - 1) / (uint32_t)parts, 1u);
     if (c.B == 1) return;
     // every entry but one may round up: at total / (parts - (B - 1)) they fit.
@@ -90,8 +104,8 @@ struct Parts {
   __device__ __forceinline__ int count(int B) const {
     if (c.B == 1) return B == 1 ? parts_of(uniform(own_steps), per) : 0;
     int used = 0;
-    for (int b0 = 0; b0 < B; b0 += 64) used += wave_sum_i(parts_of(at(b0, B), per));
-    return uniform(used);
+    for (int b0 = 0; b0 < B; b0 += 64) used += sum(parts_of(at(b0, B), per));
+    return used;
   }
   struct Found {
     int b, first, last, count;  // entry (-1: none), its steps [first, last), its parts
@@ -111,12 +125,7 @@ struct Parts {
     }
     for (int b0 = 0; b0 < c.B; b0 += 64) {
       const int st = at(b0, c.B), n = parts_of(st, per);
-      int upto = n;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(upto, o);
-        if (lane >= o) upto += y;
-      }
+      const int upto = wave_upto(n);
       const uint64_t over = __ballot(upto > slot);
       if (over) {
         const int l = (int)__builtin_ctzll(over);

@@ -141,12 +141,7 @@ __device__ __forceinline__ void hist_add(Hist& h, const bool* on, const int* dig
 // of 1024 has the counts hi and lo of the digits 2047 - 2 t and 2046 - 2 t.
 __device__ __forceinline__ void hist_find(Hist& h, int hi, int lo, int need) {
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, own = hi + lo;
-  int upto = own;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(upto, o);
-    if (lane >= o) upto += y;
-  }
+  int upto = wave_upto(own);
   if (lane == 63) h.wsum[wv] = upto;
   __syncthreads();
   for (int x = 0; x < wv; ++x) upto += h.wsum[x];
@@ -424,16 +419,10 @@ __global__ __launch_bounds__(1024) void k_evict_list(CacheCall c, EvictWork w, i
     nm += in && !mine && d >= digit && j + e >= budget;
   }
   // (a slot past the end has digit 0 and is none of these)
-  int upto = nl;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(upto, o);
-    if (lane >= o) upto += y;
-  }
-  nf = wave_sum_i(nf);
-  nm = wave_sum_i(nm);
-  if (lane == 0) freed[wv] = nf, moving[wv] = nm;
-  if (lane == 63) listed[wv] = upto;
+  const int upto = wave_upto(nl);
+  nf = wave_upto(nf);
+  nm = wave_upto(nm);
+  if (lane == 63) freed[wv] = nf, moving[wv] = nm, listed[wv] = upto;
   __syncthreads();
   if (tid == 0) {
     int f = 0, m = 0, l = 0;
@@ -545,12 +534,7 @@ __global__ __launch_bounds__(1024) void k_evict_settle(CacheCall c, EvictWork w,
     });
     __syncthreads();
     const int f = own.x + hist.bin[tid * 2][0], m = own.y + hist.bin[tid * 2 + 1][0];
-    int uf = f, um = m;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int yf = __shfl_up(uf, o), ym = __shfl_up(um, o);
-      if (lane >= o) uf += yf, um += ym;
-    }
+    const int uf = wave_upto(f), um = wave_upto(m);
     if (lane == 63) wsum[0][wv] = uf, wsum[1][wv] = um;
     __syncthreads();
     int af = base_f + uf - f, am = base_m + um - m;
@@ -595,12 +579,7 @@ __global__ __launch_bounds__(1024) void k_evict_number(CacheCall c, EvictWork w,
     nf += f[e];
     nm += m[e];
   }
-  int uf = nf, um = nm;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int yf = __shfl_up(uf, o), ym = __shfl_up(um, o);
-    if (lane >= o) uf += yf, um += ym;
-  }
+  const int uf = wave_upto(nf), um = wave_upto(nm);
   if (lane == 63) freed[wv] = uf, moving[wv] = um;
   __syncthreads();
   int af = base.x + uf - nf, am = base.y + um - nm;

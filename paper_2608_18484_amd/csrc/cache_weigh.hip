@@ -34,13 +34,16 @@ struct WeighCut {
   float* sums;     // [parts_max][B Hkv][cap]
 };
 
-// Row parts: the number whose blocks fill the chip a whole number of times best.
-__device__ __forceinline__ int weigh_parts(const CacheCall& c, const WeighCut& w, int keys, int lane) {
-  if (w.parts_max == 1) return 1;
-  int used = 0;
-  for (int b0 = 0; b0 < c.B; b0 += 64)
-    used += wave_sum_i(b0 + lane < c.B ? (cache_length(c, b0 + lane) + keys - 1) / keys : 0);
-  used = uniform(used) * c.Hkv;
+// The entries' blocks of keys, numbered over all entries (parts of one step).
+__device__ __forceinline__ auto key_blocks(const CacheCall& c, int keys, int lane) {
+  auto all = cut_parts(c, 0, c.C, lane, [keys](Entry e) { return (e.len + keys - 1) / keys; });
+  all.per = 1;
+  return all;
+}
+
+// Row parts of `used` blocks of keys: the number whose blocks fill the chip a
+// whole number of times best.
+__device__ __forceinline__ int weigh_parts(const WeighCut& w, int used) {
   int best = 1;
   for (int p = 2; p <= w.parts_max; ++p) {
     const int64_t now = (used * (int64_t)p + w.room - 1) / w.room, was = (used * (int64_t)best + w.room - 1) / w.room;
@@ -123,15 +126,19 @@ __global__ __launch_bounds__(256, weigh_blocks(D, sizeof(E) == 2)) void k_cache_
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
 
-  // XCD x takes the x-th eighth of the blocks: its L2 holds few heads' rows
-  const int parts = weigh_parts(c, w, KEYS, lane);
-  const uint32_t total = (uint32_t)(c.B * c.Hkv) * (uint32_t)(parts * w.key_blocks), eighth = (total + 7) / 8;
+  // XCD x takes the x-th eighth of the blocks in use, an entry's head by head:
+  // its L2 holds few heads' rows
+  const auto all = key_blocks(c, KEYS, lane);
+  const int used = all.count(c.B), parts = weigh_parts(w, used * c.Hkv);
+  const uint32_t each = (uint32_t)(c.Hkv * parts), total = (uint32_t)used * each, eighth = (total + 7) / 8;
   const uint32_t at = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
   if ((blockIdx.x >> 3) >= eighth || at >= total) return;
-  const int unit = (int)(at / (uint32_t)w.key_blocks), kb = (int)at - unit * w.key_blocks;
-  const int bh = unit / parts, part = unit - bh * parts, b = bh / c.Hkv, hk = bh % c.Hkv;
-  const int len = cache_length(c, b), ntok = cache_count(c, b, c.C);
-  if (kb * KEYS >= len) return;
+  const int unit = (int)(at / each);
+  const auto own = all.find(unit);
+  if (own.b < 0) return;  // (only if lengths change during the launch)
+  const int local = (int)(at - (uint32_t)(unit - own.first) * each), kb = local % own.count, hp = local / own.count;
+  const int part = hp % parts, b = own.b, hk = hp / parts, bh = b * c.Hkv + hk;
+  const int len = own.e.len, ntok = own.e.n;
   const int tiles = (ntok * c.G + 31) / 32;
   const int t_first = (int)((int64_t)tiles * part / parts), t_last = (int)((int64_t)tiles * (part + 1) / parts);
 
@@ -370,7 +377,7 @@ __global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w
 // The row parts' sums, in their order, into the scores.
 __global__ __launch_bounds__(256) void k_cache_weigh_join(CacheCall c, WeighCut w, int keys) {
   const int bh = blockIdx.y, len = cache_length(c, bh / c.Hkv), j = blockIdx.x * 256 + threadIdx.x;
-  const int parts = weigh_parts(c, w, keys, threadIdx.x & 63);
+  const int parts = weigh_parts(w, key_blocks(c, keys, threadIdx.x & 63).count(c.B) * c.Hkv);
   if (j >= len) return;
   const size_t o = (size_t)bh * c.cap + j, step = (size_t)c.B * c.Hkv * c.cap;
   float v = 0.f;

@@ -478,9 +478,11 @@ __global__ __launch_bounds__(1024) void k_evict_settle(CacheCall c, EvictWork w,
     for (int i0 = 0; i0 < n; i0 += 8192) {
       uint2 x[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = cand[min(i0 + u * 1024 + tid, n - 1)];
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u * 1024 < n) x[u] = cand[min(i0 + u * 1024 + tid, n - 1)];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) f(i0 + u * 1024 + tid < n, x[u]);
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u * 1024 < n) f(i0 + u * 1024 + tid < n, x[u]);
     }
   };
   for (int pass = 0; pass < 5 && same > need; ++pass) {

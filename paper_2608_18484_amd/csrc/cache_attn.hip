@@ -2,7 +2,7 @@
 //
 // Rows.  The G query heads of a K/V head and the T new tokens are rows
 // r = t * G + g of one product against the same keys; a block owns a tile of
-// 32 RS of them.
+// 32 RS of them (fp32: RS = 1).
 // Keys.  An entry's keys come in tiles of 32: first those of the slots in use,
 // then those of the new tokens, whose visibility is a word of 32 bits per row
 // and tile (a tree's ancestors, a chain's predecessors).  A block walks a
@@ -140,6 +140,23 @@ __device__ __forceinline__ uint32_t seen_keys(const CacheCall& c, const Where& w
   return k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1;
 }
 
+// One pass over the keys with a running maximum m and sum l of every row:
+//   p_j = 2^(s_j - m),  l = sum p_j,  O = sum p_j v_j,  out = O / l,
+// s in units of log 2; when m grows by a, l and O shrink by 2^-a.
+//
+// What bounds it.  Up to 32 rows the keys and values: four entries of up to
+// 84,480 slots are 1.13 GB, read once, 195 us (5.8 TB/s).  Then the work per key:
+// 189 rows over two entries of 75,600 slots 141 us (92 GFLOP, 0.54 GB).  A
+// frame's 4,680 rows over 18,720 keys, 344 GFLOP, take 400 us (860 TFLOP/s): the
+// matrix cores are busy 41% of the time beside 5.8 vector instructions per
+// product, LDS 17%; without the exponentials it would be 5% less, without the
+// copies 12%, without the reads of V or of K 4% each, so that no one of them is
+// the limit.  A third and a fourth copy buffer changed nothing (444 and 434 us
+// at the time), blocks of three waves and 96 rows were slower (229 and 180 us for
+// the 189 rows).
+//
+// RS sets of 32 rows share a tile's copies and barriers; with RS = 1 a wave copies
+// its own tiles and never waits for another.
 template <int D, int RS>
 __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_attend(CacheCall c, Cut cut) {
   constexpr int KS = 4 / RS;
@@ -456,24 +473,26 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
 // contracts the keys of score register e of both halves, V^T row m of block db
 // being channel m NDB + db, so that one load of a value row serves all blocks.
 // Operands go straight from memory to registers: a load feeds 256 matrix
-// cycles, so four waves ask for at most 16 bytes a clock.
-template <int D, int RS>
+// cycles, so four waves ask for at most 16 bytes a clock.  Bound by the matrix
+// cores where rows are many (189 rows over two entries of 75,600 slots, d = 128:
+// 1,122 us, 82 TFLOP/s), by memory where they
+// are few (3 rows over four entries of 84,480 slots 465 us, 4.8 TB/s).
+template <int D>
 __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(CacheCall c, Cut cut) {
-  constexpr int KS = 4 / RS;
+  constexpr int KS = 4;
   constexpr int NQ = D / 8, HQ = NQ / 2, NDB = D / 32;
   typedef float fv __attribute__((ext_vector_type(NDB)));
-  __shared__ fv red[KS > 1 ? 4 : 1][16][64];
-  __shared__ float2 ml[KS > 1 ? 4 : 1][64];
+  __shared__ fv red[KS][16][64];
+  __shared__ float2 ml[KS][64];
   __shared__ Tree tree;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
-  const int rs = wv % RS, ks = wv / RS;
   Where w;
-  if (!locate(c, cut, 32 * RS, lane, w)) return;
+  if (!locate(c, cut, 32, lane, w)) return;
   if (c.mask == SPARSEPR_TOKENS_TREE && w.t_last > w.old_tiles) tree_bits(c, w.b, w.ntok, tree);
   const int b = w.b, hk = w.hk;
-  const int row = w.row0 + rs * 32 + n;
+  const int row = w.row0 + n;
   const bool valid = row < w.rows;
   const int tok = valid ? row / c.G : 0, hq = hk * c.G + (valid ? row % c.G : 0);
   f32x4 q[NQ];
@@ -526,7 +545,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(Cach
         O[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv[e][db], S[half * 8 + e], O[db], 0, 0, 0);
   };
   bool odd = false;
-  int i = w.t_first + ks;
+  int i = w.t_first + wv;
   if (i < w.t_last) load_k(ka, i, 0);
   for (; i < w.t_last; i += KS) {
     load_k(kb, i, 1);
@@ -579,7 +598,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(Cach
   }
   float l_tot = pair_sum(l_run);
   if (__ballot(odd)) {
-    for (i = w.t_first + ks; i < w.t_last; i += KS) {
+    for (i = w.t_first + wv; i < w.t_last; i += KS) {
       if (i < w.full_tiles) continue;
       const uint32_t see = seen_keys(c, w, tree, i, valid, tok);
       const bool old = i < w.old_tiles;
@@ -597,59 +616,45 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cache_attend_f32(Cach
   }
   const size_t at_row = ((size_t)w.slot * c.Hkv + hk) * ((size_t)c.T * c.G) + row;
   float* dst = w.parts > 1 ? cut.o + at_row * D : (float*)c.out + b * c.osb + hq * c.osh + tok * c.osn;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    fv o;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) o[db] = O[db][e];
+    red[wv][e][lane] = o;
+  }
+  ml[wv][lane] = make_float2(m_run, l_tot);
+  __syncthreads();
+  if (!valid) return;
+  float f[KS];
+  m_run = ml[0][lane].x;
+#pragma unroll
+  for (int x = 1; x < KS; ++x) m_run = fmaxf(m_run, ml[x][lane].x);
+  l_tot = 0.f;
+#pragma unroll
+  for (int x = 0; x < KS; ++x) {
+    const float2 y = ml[x][lane];
+    f[x] = __builtin_amdgcn_exp2f(y.x - m_run);
+    l_tot += y.y * f[x];
+  }
   // register e of all blocks: NDB neighbouring channels
-  auto store = [&](int e, fv o, float l) {
-    if (w.parts == 1) {
 #pragma unroll
-      for (int db = 0; db < NDB; ++db) o[db] /= l;
-    }
-    *(fv*)(dst + ((e >> 2) * 8 + 4 * h + (e & 3)) * NDB) = o;
-  };
-  if constexpr (KS > 1) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      fv o;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) o[db] = O[db][e];
-      red[wv][e][lane] = o;
-    }
-    ml[wv][lane] = make_float2(m_run, l_tot);
-    __syncthreads();
-    if (!valid) return;
-    float f[KS];
-    m_run = ml[rs][lane].x;
-#pragma unroll
-    for (int x = 1; x < KS; ++x) m_run = fmaxf(m_run, ml[x * RS + rs][lane].x);
-    l_tot = 0.f;
+  for (int r = 0; r < 16 / KS; ++r) {
+    const int e = wv * (16 / KS) + r;
+    fv o{};
 #pragma unroll
     for (int x = 0; x < KS; ++x) {
-      const float2 y = ml[x * RS + rs][lane];
-      f[x] = __builtin_amdgcn_exp2f(y.x - m_run);
-      l_tot += y.y * f[x];
+      const fv y = red[x][e][lane];
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) o[db] += y[db] * f[x];
     }
+    if (w.parts == 1) {
 #pragma unroll
-    for (int r = 0; r < 16 / KS; ++r) {
-      const int e = ks * (16 / KS) + r;
-      fv o{};
-#pragma unroll
-      for (int x = 0; x < KS; ++x) {
-        const fv y = red[x * RS + rs][e][lane];
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) o[db] += y[db] * f[x];
-      }
-      store(e, o, l_tot);
+      for (int db = 0; db < NDB; ++db) o[db] /= l_tot;
     }
-  } else {
-    if (!valid) return;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      fv o;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) o[db] = O[db][e];
-      store(e, o, l_tot);
-    }
+    *(fv*)(dst + ((e >> 2) * 8 + 4 * h + (e & 3)) * NDB) = o;
   }
-  if (ks > 0 || h > 0) return;
+  if (wv > 0 || h > 0) return;
   if (w.parts > 1)
     cut.ml[at_row] = make_float2(m_run, l_tot);
   else if (c.lse)
@@ -726,30 +731,40 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheCall c, Cut cut) {
   if (i == 0 && c.lse) c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// Sets of 32 rows of a block.  One where that holds all rows: four waves then
-// stream four key tiles, which a step waits for alone.  Else four, or two where
-// an odd number of 64-row tiles would leave half a 128-row tile empty (189 rows
-// over two caches of 75,600 slots 64 us, with four sets 69; 576 rows 67.1 and
-// 68.1) and the rows are few: many rows read the keys from L2 once more for
-// every tile (4,680 rows over 18,720 keys 430 us, with two sets 459).  One set
-// for fp32's few rows: 3 over 84,480 slots 598 us, with two 1,114; for bf16's it
-// is 237 and 238.
+// Sets of 32 rows of a block.
+//
+// fp32: one.  Its waves share no copies, so that larger blocks would only round the
+// rows up further (87 rows over 20,000 slots at d = 128 99 us, with two or four
+// sets 111 and 112; 189 rows over two caches of 75,600 1,123, 1,117 and 1,403).
+//
+// bf16: one where that holds all rows, and where three hold them and the cache is
+// small, so that reading the keys again costs less than the barriers (64 rows over
+// 50,000 slots of one head 18.0 us, with two sets 25.2; 87 rows over 75,600 slots
+// of 16 heads 154 and 137).  Else two where they hold all rows, and for up to 128
+// of a cache that is not large (4 x 8 heads of 20,000 slots 77 us, with four sets
+// 83; 2 x 8 heads of 75,600 slots 141 and 130), or where an odd number of 64-row
+// tiles would leave half a 128-row tile empty and the rows are few: many rows read
+// the keys again for every tile (189 rows over 2 x 8 heads of 20,000 slots 53 us,
+// with four sets 58; 4,680 rows over 18,720 keys 459 and 430).
 int row_sets(const CacheCall& c) {
   const int64_t rows = (int64_t)c.T * c.G;
-  if (rows <= 32) return 1;
-  return rows <= 64 || ((rows + 63) / 64 % 2 == 1 && rows <= 640) ? 2 : 4;
+  if (!c.bf16 || rows <= 32) return 1;
+  const int64_t bytes = ((int64_t)c.cap + c.T) * c.B * c.Hkv * c.d * 4;  // K and V
+  if (rows <= 96 && bytes <= 64 << 20) return 1;
+  if (rows <= 64 || (rows <= 128 && bytes <= 256 << 20)) return 2;
+  return (rows + 63) / 64 % 2 == 1 && rows <= 640 ? 2 : 4;
 }
 
 // Parts.  A CU holds one block of the 128 KB of tiles of 32-row blocks at
 // d = 128 (or of fp32's registers) and two of the others (d = 64, two caches of
 // 20,000 slots: 22.5 us with two, 24.5 with one; fp32 over four of 84,480 267 and
 // 345).  The parts of an entry end together when a launch fills the chip a whole
-// number of times, so that there are at most as many as r rounds hold.  More
-// rounds than one where a part is then shorter by a twelfth: a round begins with
-// some 5 us that read nothing (a frame's 296 blocks: one part each 513 us, 3 parts
-// in two rounds 432, 5 in three 430; 24 blocks: 21 parts 156, 42 in two rounds
-// 168).  fp32's parts take so long that a 25th will do (24 blocks: 10 parts
-// 1,243 us, 21 in two rounds 1,121).
+// number of times, so that there are at most as many as r rounds of blocks hold:
+// the r whose rounds are shortest together, each of a part's keys and of a start
+// that takes as long as some 500 keys (a frame's 296 blocks: one part each 513 us,
+// 3 parts in two rounds 432, 5 in three 430; 24 blocks over two caches of 75,600
+// slots: 21 parts 151, 42 in two rounds 173; 1,400 rows of 16 heads over 5,000
+// slots: 109 in parts of several rounds, 132 in one).
 //
 // Few keys are one part, done before a second kernel would have joined several:
 // one token over 700 slots 14.1 us, in parts 15.4, over 1,021 17.1 and 15.4; 189
@@ -764,12 +779,15 @@ Cut make_cut(const CacheCall& c) {
   cut.slots = c.B;
   if ((int64_t)c.cap + c.T <= (c.bf16 ? 768 : 128)) return cut;
   const int64_t units = (int64_t)c.Hkv * cut.row_tiles;  // blocks of a part
-  const int64_t room = c.d == 128 && (rs == 1 || !c.bf16) ? 256 : 512;
-  double best = 1e30;
-  for (int r = 1; r <= 4; ++r) {
+  const int64_t room = c.d == 128 && rs == 1 ? 256 : 512;
+  const double keys = (double)c.cap + c.T, start = 500;
+  double best = (c.B * units + room - 1) / room * (keys + start);
+  for (int r = 1; r <= 8; ++r) {
     const int64_t parts = r * room / units;
-    if (parts <= c.B || r / (double)parts >= best * (c.bf16 ? 0.92 : 0.96)) continue;
-    best = r / (double)parts;
+    if (parts <= c.B) continue;
+    const double cost = r * (keys * c.B / (parts - 0.5 * (c.B - 1)) + start);
+    if (cost >= best) continue;
+    best = cost;
     cut.slots = (int)parts;
     cut.split = 1;
   }
@@ -782,17 +800,14 @@ template <int D>
 void attend(const CacheCall& c, const Cut& cut, hipStream_t s) {
   const int64_t blocks = ((int64_t)cut.slots * c.Hkv * cut.row_tiles + 7) / 8 * 8;
   const dim3 grid((unsigned)blocks);
-  auto sets = [&](auto rs) {
-    if (c.bf16)
-      k_cache_attend<D, rs.value><<<grid, 256, 0, s>>>(c, cut);
-    else
-      k_cache_attend_f32<D, rs.value><<<grid, 256, 0, s>>>(c, cut);
-  };
-  switch (row_sets(c)) {
-    case 1: sets(std::integral_constant<int, 1>{}); break;
-    case 2: sets(std::integral_constant<int, 2>{}); break;
-    default: sets(std::integral_constant<int, 4>{});
-  }
+  if (!c.bf16)
+    k_cache_attend_f32<D><<<grid, 256, 0, s>>>(c, cut);
+  else if (cut.ks == 4)
+    k_cache_attend<D, 1><<<grid, 256, 0, s>>>(c, cut);
+  else if (cut.ks == 2)
+    k_cache_attend<D, 2><<<grid, 256, 0, s>>>(c, cut);
+  else
+    k_cache_attend<D, 4><<<grid, 256, 0, s>>>(c, cut);
   if (!cut.split) return;
   const int64_t heads = (int64_t)c.B * c.Hkv, R = (int64_t)c.T * c.G;
   auto join = [&](auto alone) {

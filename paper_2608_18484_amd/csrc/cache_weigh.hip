@@ -111,6 +111,15 @@ __global__ __launch_bounds__(256) void k_cache_weigh_rows(CacheCall c, WeighCut 
 constexpr int weigh_blocks(int d, bool bf16) { return d == 128 && !bf16 ? 2 : 3; }
 
 // E: element type; SETS: sets of 32 keys of a wave.
+//
+// Bound by the vector units beside the matrix cores: an exponential, a
+// subtraction and an addition for each of a product's 16 scores a lane, 7.7 vector
+// instructions per product.  A frame's 4,680 rows over 18,720 slots of 8 heads,
+// 172 GFLOP, 192 us (900 TFLOP/s, matrix cores 44% busy, 6.4 us more to gather the
+// rows and as much to join the parts).  With rows gathered by every block for itself
+// the call took 388 us where it then took 225, with two blocks a CU 225 and with
+// three 210; a next tile's products beside this one's exponentials need registers
+// that leave two blocks, 225 to 246.
 template <int D, class E, int SETS>
 __global__ __launch_bounds__(256, weigh_blocks(D, sizeof(E) == 2)) void k_cache_accumulate(CacheCall c, WeighCut w) {
   constexpr int EPC = 16 / sizeof(E);       // elements of a 16-byte chunk
@@ -269,7 +278,8 @@ __global__ __launch_bounds__(256, weigh_blocks(D, sizeof(E) == 2)) void k_cache_
 
 // At most 32 rows: their operands stay in registers and the keys stream by.
 // Every wave walks key tiles of its own through LDS, NB of them on the way by
-// direct copies, so that the launch runs at the rate at which K arrives; the
+// direct copies, so that the launch runs at the rate at which K arrives (18 rows
+// over four caches of up to 84,480 slots, 572 MB, 115 us: 5.0 TB/s); the
 // slots' scores come along with the keys (a load of their own would wait for
 // the copies behind it).
 template <int D, class E>
@@ -385,7 +395,7 @@ __global__ __launch_bounds__(256) void k_cache_weigh_join(CacheCall c, WeighCut 
   c.scores[o] += v;
 }
 
-constexpr int kRoom = 256;  // blocks of k_cache_weigh_few aimed at
+constexpr int kRoom = 256;  // blocks of k_cache_weigh_few: one a CU
 
 constexpr int weigh_keys(bool bf16) { return bf16 ? 256 : 128; }
 

@@ -455,7 +455,9 @@ sparsepr_status sparsepr_cache_append(const sparsepr_cache* cache, const sparsep
  * to the slots j <= L - c + i (CAUSAL and TREE) or j < L (FULL).  q and lse are
  * those of the attend call.  To weigh by the last tokens of a prompt only, pass
  * these alone.  Each slot's sum is taken in a fixed order: the same inputs give
- * the same scores.  Rows whose lse is -inf add nothing. */
+ * the same scores.  Rows whose lse is -inf add nothing.  Rows of an entry whose
+ * append was refused (its flag) sit in no slot: weigh that entry with counts[b] = 0.
+ * An index outside [0, n) raises the flag of entries that have slots in use. */
 sparsepr_status sparsepr_cache_accumulate_workspace_size(const sparsepr_cache* cache,
                                                          const sparsepr_tokens* tokens,
                                                          int32_t n_rows, size_t* bytes);

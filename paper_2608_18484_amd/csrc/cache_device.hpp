@@ -39,6 +39,17 @@ __device__ __forceinline__ int wave_upto(int x) {
   return x;
 }
 
+// The wave's largest value, by the same moves.
+__device__ __forceinline__ int wave_largest(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
 // The work of a launch, cut into parts of equal length over all entries.  An
 // entry has some steps, known on the device alone; a part is `per` consecutive
 // ones of an entry (the last part of an entry is shorter), and the parts are

@@ -121,6 +121,14 @@ __device__ __forceinline__ i32x4_u four(const int32_t* p, int j, int len) {
   return v;
 }
 
+// Of 16 values that a block's waves left in LDS: the sum of those before wave
+// `wv`, and of all.
+__device__ __forceinline__ int before_wave(const int* w, int wv, int lane, int& all) {
+  const int upto = wave_upto(lane < 16 ? w[lane] : 0);
+  all = __builtin_amdgcn_readlane(upto, 15);
+  return wv ? __builtin_amdgcn_readlane(upto, wv - 1) : 0;
+}
+
 // A histogram of a digit in LDS, in copies so that equal digits of neighbouring
 // lanes do not meet.
 constexpr int kCopies = 4;
@@ -149,11 +157,11 @@ __device__ __forceinline__ void hist_add(Hist& h, const bool* on, const int* dig
 // of its keys are then needed (h.need) and how many there are (h.same).  Thread t
 // of 1024 has the counts hi and lo of the digits 2047 - 2 t and 2046 - 2 t.
 __device__ __forceinline__ void hist_find(Hist& h, int hi, int lo, int need) {
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, own = hi + lo;
-  int upto = wave_upto(own);
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), own = hi + lo;
+  int upto = wave_upto(own), all;
   if (lane == 63) h.wsum[wv] = upto;
   __syncthreads();
-  for (int x = 0; x < wv; ++x) upto += h.wsum[x];
+  upto += before_wave(h.wsum, wv, lane, all);
   if (upto >= need && upto - own < need) {
     const int left = need - (upto - own);
     h.digit = left <= hi ? kBins - 1 - 2 * tid : kBins - 2 - 2 * tid;
@@ -177,10 +185,11 @@ constexpr int kTurns = 6, kSmall = kTurns * 4096;
 // Every wave has a run of neighbouring slots and a lane four neighbours of each
 // 256.  All of its scores and positions are read at once, so that memory is
 // waited for once, and the digits' passes go over registers; the numbering needs
-// one exchange between the waves.  What bounds it is one CU's issue of some 60
-// instructions a slot: 17,160 slots of 32 heads 25 us.  Keys that every pass read
-// again from L2 took 31; runs of neighbouring slots a thread, numbered by a scan
-// over the threads instead of ballots, 29: their loads and stores scatter.
+// one exchange between the waves.  17,160 slots of 32 heads 23 us: 84 vector
+// instructions a slot on one CU are two fifths of that, the rest is the phases' waits
+// for memory and for each other.  Keys that every pass read again from L2 took 31;
+// runs of neighbouring slots a thread, numbered by a scan over the threads instead
+// of ballots, 29: their loads and stores scatter.
 __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w, int in_place, int budget, int n_sink, int n_recent) {
   __shared__ Hist hist;
   __shared__ int wsum[3][16], sh_newest;
@@ -216,8 +225,7 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
     if (n_recent > 0) {
 #pragma unroll
       for (int i = 0; i < kTurns; ++i) newest = max(newest, max(max(p[i].x, p[i].y), max(p[i].z, p[i].w)));
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) newest = max(newest, __shfl_xor(newest, o));
+      newest = wave_largest(newest);
       if (lane == 0) atomicMax(&sh_newest, newest);
       __syncthreads();
       newest = sh_newest;
@@ -278,7 +286,8 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
     });
     if (lane == 0) wsum[0][wv] = n_eq;
     __syncthreads();
-    for (int x = 0; x < wv; ++x) eq0 += wsum[0][x];
+    int all;
+    eq0 = before_wave(wsum[0], wv, lane, all);
   }
   // f(first slot, freed, moves, ballots of both) in the order of the slots
   auto number = [&](auto&& f) {
@@ -317,11 +326,8 @@ __global__ __launch_bounds__(1024) void k_evict_select(CacheCall c, EvictWork w,
   });
   if (lane == 0) wsum[1][wv] = n_hole, wsum[2][wv] = n_move;
   __syncthreads();
-  int at_hole = 0, at_move = 0, moves_all = 0;
-  for (int x = 0; x < 16; ++x) {
-    if (x < wv) at_hole += wsum[1][x], at_move += wsum[2][x];
-    moves_all += wsum[2][x];
-  }
+  int holes_all, moves_all;
+  int at_hole = before_wave(wsum[1], wv, lane, holes_all), at_move = before_wave(wsum[2], wv, lane, moves_all);
   number([&](int j, const bool* freed, const bool* moves, const uint64_t* bf, const uint64_t* bm) {
     int rf = at_hole + ahead(bf), rm = at_move + ahead(bm);
 #pragma unroll
@@ -350,13 +356,12 @@ __global__ __launch_bounds__(1024) void k_evict_newest(CacheCall c, EvictWork w,
     const i32x4_u p = four(c.positions + (size_t)bh * c.cap, j, len);
     m = max(max(p.x, p.y), max(p.z, p.w));
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o));
+  m = wave_largest(m);
   if ((tid & 63) == 0) best[tid >> 6] = m;
   __syncthreads();
-  if (tid > 0) return;
-  for (int x = 1; x < 16; ++x) m = max(m, best[x]);
-  w.newest[(size_t)bh * w.blocks + blk] = m;
+  if (tid >= 64) return;
+  m = wave_largest(best[tid & 15]);
+  if (tid == 0) w.newest[(size_t)bh * w.blocks + blk] = m;
 }
 
 // The keys, and the head's histogram of their first digits.
@@ -374,8 +379,7 @@ __global__ __launch_bounds__(1024) void k_evict_keys(CacheCall c, EvictWork w, i
   int newest = INT_MIN;
   if (n_recent > 0) {
     for (int x = lane; x * kSlots < len; x += 64) newest = max(newest, w.newest[(size_t)bh * w.blocks + x]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) newest = max(newest, __shfl_xor(newest, o));
+    newest = wave_largest(newest);
   }
   hist_clear(hist);
   uint32_t k[4];
@@ -410,7 +414,8 @@ __device__ __forceinline__ uint4 block_keys(const EvictWork& w, int bh, int j, i
 __global__ __launch_bounds__(1024) void k_evict_list(CacheCall c, EvictWork w, int budget) {
   __shared__ Hist hist;
   __shared__ int freed[16], moving[16], listed[16], at;
-  const int bh = blockIdx.x / w.blocks, blk = blockIdx.x % w.blocks, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int bh = blockIdx.x / w.blocks, blk = blockIdx.x % w.blocks, tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = cache_length(c, bh / c.Hkv), j = blk * kSlots + tid * 4;
   if (len <= budget || blk * kSlots >= len) return;
   const uint4 k4 = block_keys(w, bh, j, len);
@@ -433,15 +438,19 @@ __global__ __launch_bounds__(1024) void k_evict_list(CacheCall c, EvictWork w, i
   nm = wave_upto(nm);
   if (lane == 63) freed[wv] = nf, moving[wv] = nm, listed[wv] = upto;
   __syncthreads();
-  if (tid == 0) {
-    int f = 0, m = 0, l = 0;
-    for (int x = 0; x < 16; ++x) f += freed[x], m += moving[x], l += listed[x];
-    w.part[(size_t)bh * w.blocks + blk] = make_int2(f, m);
-    at = l ? atomicAdd(&w.state[bh].x, l) : 0;
+  int l;
+  int put = before_wave(listed, wv, lane, l) + upto - nl;
+  if (wv == 0) {
+    int f, m;
+    (void)before_wave(freed, 0, lane, f);
+    (void)before_wave(moving, 0, lane, m);
+    if (lane == 0) {
+      w.part[(size_t)bh * w.blocks + blk] = make_int2(f, m);
+      at = l ? atomicAdd(&w.state[bh].x, l) : 0;
+    }
   }
   __syncthreads();
-  int put = at + upto - nl;
-  for (int x = 0; x < wv; ++x) put += listed[x];
+  put += at;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (j + e < len && open && (int)(k[e] >> 21) == digit) w.cand[(size_t)bh * w.cap_pad + put++] = make_uint2(k[e], (uint32_t)(j + e));
@@ -467,7 +476,8 @@ __device__ __forceinline__ void count_at(Hist& h, bool on, int at, int copy, int
 __global__ __launch_bounds__(1024) void k_evict_settle(CacheCall c, EvictWork w, int budget) {
   __shared__ Hist hist;
   __shared__ int wsum[2][16];
-  const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = cache_length(c, bh / c.Hkv);
   if (len <= budget) {
     if (tid == 0) w.count[bh] = make_int2(0, len);
@@ -548,12 +558,11 @@ __global__ __launch_bounds__(1024) void k_evict_settle(CacheCall c, EvictWork w,
     const int uf = wave_upto(f), um = wave_upto(m);
     if (lane == 63) wsum[0][wv] = uf, wsum[1][wv] = um;
     __syncthreads();
-    int af = base_f + uf - f, am = base_m + um - m;
-    for (int y = 0; y < 16; ++y) {
-      if (y < wv) af += wsum[0][y], am += wsum[1][y];
-      base_f += wsum[0][y];
-      base_m += wsum[1][y];
-    }
+    int all_f, all_m;
+    const int af = base_f + before_wave(wsum[0], wv, lane, all_f) + uf - f;
+    const int am = base_m + before_wave(wsum[1], wv, lane, all_m) + um - m;
+    base_f += all_f;
+    base_m += all_m;
     if (x < blocks) part[x] = make_int2(af, am);
     __syncthreads();
   }
@@ -566,7 +575,8 @@ __global__ __launch_bounds__(1024) void k_evict_settle(CacheCall c, EvictWork w,
 // The freed and the moving slots at their places.
 __global__ __launch_bounds__(1024) void k_evict_number(CacheCall c, EvictWork w, int in_place, int budget) {
   __shared__ int freed[16], moving[16];
-  const int bh = blockIdx.x / w.blocks, blk = blockIdx.x % w.blocks, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int bh = blockIdx.x / w.blocks, blk = blockIdx.x % w.blocks, tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = cache_length(c, bh / c.Hkv), j = blk * kSlots + tid * 4;
   if (blk * kSlots >= len) return;
   int32_t* stay = w.stay + (size_t)bh * budget;
@@ -593,8 +603,8 @@ __global__ __launch_bounds__(1024) void k_evict_number(CacheCall c, EvictWork w,
   const int uf = wave_upto(nf), um = wave_upto(nm);
   if (lane == 63) freed[wv] = uf, moving[wv] = um;
   __syncthreads();
-  int af = base.x + uf - nf, am = base.y + um - nm;
-  for (int x = 0; x < wv; ++x) af += freed[x], am += moving[x];
+  int all;
+  int af = base.x + before_wave(freed, wv, lane, all) + uf - nf, am = base.y + before_wave(moving, wv, lane, all) + um - nm;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     if (f[e]) w.hole[(size_t)bh * budget + af++] = j + e;

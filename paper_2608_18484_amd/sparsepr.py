@@ -411,15 +411,15 @@ def _tensor(name, t, shape, dtype, device, contiguous=True):
     contiguous or with a contiguous last dimension."""
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if t.device == device and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return
     if t.device != device:
         raise ValueError(f"{name}: tensor on {t.device}, the cache is on {device}")
     if t.dtype is not dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.is_contiguous():
-        return
-    if contiguous:
+    if contiguous and not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: last dimension must be contiguous")
@@ -498,7 +498,8 @@ class KVCache:
         where they are not, so that scratch memory and outputs made by the call
         belong to the stream that uses them."""
         if stream is None:
-            handle = torch.cuda.current_stream(self.device).cuda_stream
+            # (the handle alone: the stream object takes longer than a short kernel's launch)
+            handle = torch._C._cuda_getCurrentRawStream(self.device.index)
             if self.device.index == torch.cuda.current_device():
                 return launch(handle)
             with torch.cuda.device(self.device):

@@ -767,9 +767,9 @@ int row_sets(const CacheCall& c) {
 // slots: 109 in parts of several rounds, 132 in one).
 //
 // Few keys are one part, done before a second kernel would have joined several:
-// one token over 700 slots 14.1 us, in parts 15.4, over 1,021 17.1 and 15.4; 189
-// rows of 16 heads over 700 17.5 and 22.5, over 1,021 20.9 and 24.8; fp32 over
-// 100 slots 16.2 and 15.9, over 300 21.1 and 15.4.
+// one token over 512 slots 12.6 us, in parts 13.8, over 768 14.4 and 13.8; 189
+// rows of 16 heads over 512 14.0 and 22.0; fp32 over 60 slots 11.2 and 13.9, over
+// 150 16.2 and 14.8.
 Cut make_cut(const CacheCall& c) {
   Cut cut{};
   const int rs = row_sets(c);
@@ -777,7 +777,7 @@ Cut make_cut(const CacheCall& c) {
   cut.ks = 4 / rs;
   cut.row_tiles = (int)((rows + 32 * rs - 1) / (32 * rs));
   cut.slots = c.B;
-  if ((int64_t)c.cap + c.T <= (c.bf16 ? 768 : 128)) return cut;
+  if ((int64_t)c.cap + c.T <= (c.bf16 ? 640 : 128)) return cut;
   const int64_t units = (int64_t)c.Hkv * cut.row_tiles;  // blocks of a part
   const int64_t room = c.d == 128 && rs == 1 ? 256 : 512;
   const double keys = (double)c.cap + c.T, start = 500;

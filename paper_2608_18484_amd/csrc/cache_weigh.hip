@@ -300,27 +300,6 @@ __global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w
   const int b = part.b, len = part.e.len, ntok = part.e.n;
   const int rows = ntok * c.G;
   if (rows == 0) return;
-  // this lane's row of the operand; the rows of its score registers
-  int tok;
-  int sees = row_sees(c, b, len, ntok, n / c.G, part.first == 0 && hk == 0, tok);
-  const int hq = hk * c.G + n % c.G;
-  uint4 q[NF];
-  {
-    const E* src = (const E*)c.q + b * c.qsb + hq * c.qsh + tok * c.qsn + h * EPC;
-#pragma unroll
-    for (int x = 0; x < NF; ++x) q[x] = *(const uint4*)(src + x * 2 * EPC);
-  }
-  float z = c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok];
-  if (z == -INFINITY) sees = 0;
-  if (sees == 0) z = 0.f;
-  float zr[16];
-  int vr[16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int r = (e >> 2) * 8 + h * 4 + (e & 3);
-    zr[e] = __shfl(z, r) * 1.4426950408889634f;
-    vr[e] = __shfl(sees, r);
-  }
   const char* kc = (const char*)((const E*)c.k + b * c.sb + hk * c.sh);
   float* score = c.scores + ((size_t)b * c.Hkv + hk) * c.cap;
   const int tiles = (len + kKeys - 1) / kKeys, full_tiles = len / kKeys;
@@ -343,14 +322,35 @@ __global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w
       g2lds16s(p, (uint32_t)min(ckey[u], left) * stride + cchunk[u], k_lds + buf * (kKeys * CH * 16) + u * 1024);
     g2lds4s(score + i * kKeys, (uint32_t)min(n, left) * 4, s_lds + buf * 256);
   };
-  wait_copies<0>();
-  const float sl2 = 1.4426950408889634f / sqrtf((float)D);
   int i = part.first * 4 + wv;
   // a wave always has NB tiles under way; those past its last repeat it
   const int i_last = i < t_last ? i + (t_last - 1 - i) / 4 * 4 : i;
   if (i >= t_last) return;
 #pragma unroll
   for (int x = 0; x < NB; ++x) issue(min(i + x * 4, i_last), x);
+  // behind the first copies: this lane's row of the operand, the rows of its score
+  // registers
+  int tok;
+  int sees = row_sees(c, b, len, ntok, n / c.G, part.first == 0 && hk == 0, tok);
+  const int hq = hk * c.G + n % c.G;
+  uint4 q[NF];
+  {
+    const E* src = (const E*)c.q + b * c.qsb + hq * c.qsh + tok * c.qsn + h * EPC;
+#pragma unroll
+    for (int x = 0; x < NF; ++x) q[x] = *(const uint4*)(src + x * 2 * EPC);
+  }
+  float z = c.lse[((size_t)b * c.Hkv * c.G + hq) * c.T + tok];
+  if (z == -INFINITY) sees = 0;
+  if (sees == 0) z = 0.f;
+  float zr[16];
+  int vr[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int r = (e >> 2) * 8 + h * 4 + (e & 3);
+    zr[e] = __shfl(z, r) * 1.4426950408889634f;
+    vr[e] = __shfl(sees, r);
+  }
+  const float sl2 = 1.4426950408889634f / sqrtf((float)D);
   for (int buf = 0; i < t_last; i += 4, buf = buf + 1 == NB ? 0 : buf + 1) {
     wait_copies<(NB - 1) * (NCP + 1)>();
     const uint4* k = kt[wv][buf];

@@ -450,7 +450,7 @@ class KVCache:
                  (evict's n_sink and n_recent)
 
     Calls are enqueued on `stream` (default: the current stream of the cache's
-    device) and never synchronise; flags() does."""
+    device) and never synchronise; flags() does.  Inference only: no gradients."""
 
     def __init__(self, k, v, lengths, scores=None, positions=None):
         global torch

@@ -415,8 +415,9 @@ typedef struct {
  *            that does not see it, whatever it holds.
  *   lse      [batch, heads, n] contiguous or NULL: log sum exp of each row's scores
  *            (natural logarithm), which sparsepr_cache_accumulate takes.
- * Sums are in float32; with bf16 inputs the weights of the V product are
- * rounded to bf16, lse is not.  `workspace` (16-byte aligned) holds
+ * Sums are in float32, over weights of at most 1 that are divided by their sum at
+ * the end; with bf16 inputs the weights of the V product are rounded to bf16, lse
+ * is not.  `workspace` (16-byte aligned) holds
  * sparsepr_cache_attend_workspace_size bytes (which depend on the geometry
  * alone) and belongs to the call until its work has completed.
  * Errors (all four operators): INVALID_ARGUMENT for bad pointers, sizes and

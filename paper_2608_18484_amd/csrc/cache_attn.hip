@@ -36,8 +36,8 @@ struct Cut {
   int ks;           // key tiles of a step
   int split;        // 0: one part per entry
   int slots;        // parts of all entries at most (of each head and row tile)
-  float* o;         // [slots][Hkv][T G][D] parts' outputs, relative to their maxima
-  float2* ml;       // [slots][Hkv][T G] maxima (base 2) and sums
+  float* o;         // [slots][Hkv][T G][D] parts' outputs, relative to their bounds
+  float2* ml;       // [slots][Hkv][T G] bounds (base 2) and sums
 };
 
 // Steps of an entry: those of its cache tiles and new tiles together.
@@ -140,7 +140,7 @@ __device__ __forceinline__ uint32_t seen_keys(const CacheCall& c, const Where& w
   return k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1;
 }
 
-// One pass over the keys with a running maximum m and sum l of every row:
+// One pass over the keys with a running bound m >= max s_j and sum l of every row:
 //   p_j = 2^(s_j - m),  l = sum p_j,  O = sum p_j v_j,  out = O / l,
 // s in units of log 2; when m grows by a, l and O shrink by 2^-a.
 //
@@ -281,10 +281,14 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
   auto finish = [&](f32x16& S, float mt, int buf, auto&& between) {
     const uint16_t* vt = kv[ks][buf][1];
     const float mp = pair_max(mt) * sl2;
-    // the running maximum moves only when a tile exceeds it by 2^8
-    const bool need = mp > m_run + 8.f;
+    // the bound moves only when a tile exceeds it, and then to 8 above that: the
+    // weights are at most 1, as those of a softmax are, and values overflow where its
+    // sum would (a maximum that lagged by 8 had weights of up to 2^8 and lost values
+    // from 1.3e36 on; one that moves with every tile takes 444 us for a frame's 415,
+    // and 162 for the 189 rows' 150)
+    const bool need = mp > m_run;
     if (__ballot(need)) {
-      const float m_new = need ? mp : m_run;
+      const float m_new = need ? mp + 8.f : m_run;
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;

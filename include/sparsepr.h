@@ -387,6 +387,10 @@ typedef struct {
 #define SPARSEPR_CACHE_FLAG_BAD_INDEX 2 /* append: a row index outside [0, n): none was appended;
                                            accumulate: such rows were left out; attend: a parent
                                            outside [-1, own index): the token was taken for a root */
+#define SPARSEPR_CACHE_FLAG_REFUSED 4   /* append sets it where it appended none of an entry's rows
+                                           and clears it where it appended them: accumulate leaves
+                                           such an entry as it is.  A caller that clears the other
+                                           flags between the two keeps this one */
 
 /* How the new tokens see each other (all of them see the whole cache). */
 #define SPARSEPR_TOKENS_CAUSAL 0 /* token t sees the tokens 0 .. t */
@@ -457,8 +461,10 @@ sparsepr_status sparsepr_cache_append(const sparsepr_cache* cache, const sparsep
  * those of the attend call.  To weigh by the last tokens of a prompt only, pass
  * these alone.  Each slot's sum is taken in a fixed order: the same inputs give
  * the same scores.  Rows whose lse is -inf add nothing.  Rows of an entry whose
- * append was refused (its flag) sit in no slot: weigh that entry with counts[b] = 0.
- * An index outside [0, n) raises the flag of entries that have slots in use. */
+ * last append was refused sit in no slot and add nothing either, as long as the
+ * cache has flags (SPARSEPR_CACHE_FLAG_REFUSED); without flags, weigh that entry
+ * with counts[b] = 0.  An index outside [0, n) raises the flag of entries that
+ * have slots in use. */
 sparsepr_status sparsepr_cache_accumulate_workspace_size(const sparsepr_cache* cache,
                                                          const sparsepr_tokens* tokens,
                                                          int32_t n_rows, size_t* bytes);

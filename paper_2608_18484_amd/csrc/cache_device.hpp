@@ -11,7 +11,10 @@ namespace sparsepr {
 __device__ __forceinline__ int cache_length(const CacheCall& c, int b) {
   return min(max(c.lengths[b], 0), c.cap);
 }
+// `appended`: rows that entered the cache, none where the append was refused.
+template <bool appended = false>
 __device__ __forceinline__ int cache_count(const CacheCall& c, int b, int most) {
+  if (appended && c.flags && (c.flags[b] & SPARSEPR_CACHE_FLAG_REFUSED)) return 0;
   return c.counts ? min(max(c.counts[b], 0), most) : most;
 }
 
@@ -66,7 +69,7 @@ struct Entry {
   int len, n;  // slots in use, tokens
 };
 
-template <class F>
+template <bool appended, class F>
 struct Parts {
   const CacheCall& c;
   int most;       // tokens of an entry at most
@@ -76,7 +79,7 @@ struct Parts {
   int own_steps;
   int per;        // steps of a part
 
-  __device__ __forceinline__ Entry entry(int b) const { return {cache_length(c, b), cache_count(c, b, most)}; }
+  __device__ __forceinline__ Entry entry(int b) const { return {cache_length(c, b), cache_count<appended>(c, b, most)}; }
   // steps of entry b0 + lane
   __device__ __forceinline__ int at(int b0, int B) const {
     if (b0 == 0) return lane < B ? own_steps : 0;
@@ -153,9 +156,9 @@ struct Parts {
     return p;
   }
 };
-template <class F>
-__device__ __forceinline__ Parts<F> cut_parts(const CacheCall& c, int parts, int most, int lane, F f) {
-  return Parts<F>(c, parts, most, lane, f);
+template <bool appended = false, class F>
+__device__ __forceinline__ Parts<appended, F> cut_parts(const CacheCall& c, int parts, int most, int lane, F f) {
+  return Parts<appended, F>(c, parts, most, lane, f);
 }
 
 template <int N>

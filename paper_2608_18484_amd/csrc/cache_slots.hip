@@ -47,7 +47,10 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheCall c, const int32_t
   int flag;
   const int n = rows_to_append(c, b, len, flag);
   if (blockIdx.x == 0 && h0 == 0 && threadIdx.x == 0) {
-    if (flag) raise_flag(c, b, flag);
+    if (flag)
+      raise_flag(c, b, flag | SPARSEPR_CACHE_FLAG_REFUSED);
+    else if (c.flags)
+      atomicAnd(c.flags + b, ~SPARSEPR_CACHE_FLAG_REFUSED);
     if (lengths_out != c.lengths || whole) lengths_out[b] = len + max(n, 0);
   }
   const int64_t per = (int64_t)n * ch;

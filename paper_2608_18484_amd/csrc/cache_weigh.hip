@@ -36,7 +36,7 @@ struct WeighCut {
 
 // The entries' blocks of keys, numbered over all entries (parts of one step).
 __device__ __forceinline__ auto key_blocks(const CacheCall& c, int keys, int lane) {
-  auto all = cut_parts(c, 0, c.C, lane, [keys](Entry e) { return (e.len + keys - 1) / keys; });
+  auto all = cut_parts<true>(c, 0, c.C, lane, [keys](Entry e) { return (e.len + keys - 1) / keys; });
   all.per = 1;
   return all;
 }
@@ -78,7 +78,7 @@ template <int D, class E>
 __global__ __launch_bounds__(256) void k_cache_weigh_rows(CacheCall c, WeighCut w) {
   constexpr int EPC = 16 / sizeof(E), CH = D / EPC;
   const int t = blockIdx.x % w.tiles_max, bh = blockIdx.x / w.tiles_max, b = bh / c.Hkv, hk = bh % c.Hkv;
-  const int len = cache_length(c, b), ntok = cache_count(c, b, c.C), tid = threadIdx.x;
+  const int len = cache_length(c, b), ntok = cache_count<true>(c, b, c.C), tid = threadIdx.x;
   if (t * 32 >= ntok * c.G) return;
   const size_t at = (size_t)bh * w.tiles_max + t;
   uint4* dst = (uint4*)w.rows + at * 32 * CH;
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256) void k_cache_weigh_few(CacheCall c, WeighCut w
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
-  const auto all = cut_parts(c, w.parts, c.C, lane, [](Entry e) { return (e.len + 4 * kKeys - 1) / (4 * kKeys); });
+  const auto all = cut_parts<true>(c, w.parts, c.C, lane, [](Entry e) { return (e.len + 4 * kKeys - 1) / (4 * kKeys); });
   const int slot = blockIdx.x / c.Hkv, hk = blockIdx.x % c.Hkv;
   const auto part = all.find(slot);
   if (part.b < 0) return;

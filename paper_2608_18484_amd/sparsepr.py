@@ -83,7 +83,7 @@ class Tokens(ctypes.Structure):
 
 
 TOKENS_CAUSAL, TOKENS_FULL, TOKENS_TREE = 0, 1, 2
-CACHE_FLAG_OVERFLOW, CACHE_FLAG_BAD_INDEX = 1, 2
+CACHE_FLAG_OVERFLOW, CACHE_FLAG_BAD_INDEX, CACHE_FLAG_REFUSED = 1, 2, 4
 HOST_FIELDS = [
     ("labels_q", "i4"), ("labels_kv", "i4"), ("routes", "u1"), ("probes", "i4"),
     ("n_probes", None),
@@ -483,13 +483,14 @@ class KVCache:
     _device_type = "cuda"
 
     def flags(self) -> list:
-        """CACHE_FLAG_* raised on the device since the last call, per batch
-        entry; clears them.  Waits for the device."""
+        """CACHE_FLAG_OVERFLOW and _BAD_INDEX raised on the device since the
+        last call, per batch entry; clears them.  Waits for the device."""
         torch.cuda.synchronize(self.device)
         got = self._flags.tolist()
-        self._flags.zero_()
+        # (append's own note for accumulate stays)
+        self._flags.bitwise_and_(CACHE_FLAG_REFUSED)
         torch.cuda.synchronize(self.device)
-        return got
+        return [x & ~CACHE_FLAG_REFUSED for x in got]
 
     # -- marshalling --------------------------------------------------------
 
@@ -616,7 +617,8 @@ class KVCache:
     def accumulate(self, q, lse, rows=None, counts=None, causal=True, stream=None):
         """Add the attention weights of the rows that were just appended (rows
         and counts as in append; q and lse as in attend) to the scores of the
-        slots that they see; see sparsepr_cache_accumulate."""
+        slots that they see; see sparsepr_cache_accumulate.  Entries whose
+        append was refused (flags()) keep their scores."""
         h, n = self._q(q)
         c = self.desc
         width = self._list(rows, counts, n)

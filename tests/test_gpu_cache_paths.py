@@ -29,3 +29,42 @@ def test_large_values_behind_a_rising_score(dtype, d, t):
     for x, y in ((c.dq, c.q), (c.dk, c.k), (c.dkn, c.kn), (c.dv, c.v)):
         x.copy_(y)
     T.run_attend(c)
+
+
+# ---- refused appends ----------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("g,t", [(1, 20), (3, 20)])
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("clear", [False, True])
+def test_rows_of_a_refused_append_weigh_nothing(dtype, g, t, in_place, clear):
+    c = Case(dtype, 64, b=3, hkv=2, g=g, cap=100, lens=(90, 40, 60), t=t, fill=0.5)
+    rows, counts = np.tile(np.arange(t), (3, 1)), [t, t, t]
+    rows[1, 3] = t
+    tpos = np.tile(200 + np.arange(t), (3, 1))
+    lse = torch.full((3, c.h, t), 3.0)
+    over, bad = S().CACHE_FLAG_OVERFLOW, S().CACHE_FLAG_BAD_INDEX
+
+    def step(rows, counts, flags):
+        c.k, c.v, c.scores, c.pos, lens, want = T.append_ref(c, rows, counts, tpos)
+        assert want == flags
+        new = None if in_place else torch.zeros_like(c.dlen)
+        c.cache.append(c.dkn, c.dvn, positions=ints(tpos), rows=ints(rows), counts=ints(counts),
+                       lengths_out=new)
+        if new is not None:
+            c.dlen.copy_(new)
+        if clear:  # the caller has seen the flags before the weights are added
+            assert c.cache.flags() == flags
+        c.lens = lens
+        on = [0 if f else n for f, n in zip(flags, counts)]
+        want, tol = T.accumulate_ref(c, lse, rows, on)
+        c.cache.accumulate(c.dq, lse.cuda(), rows=ints(rows), counts=ints(counts))
+        assert c.cache.flags() == ([0, 0, 0] if clear else flags)
+        check("scores", c.dscores, want, tol)
+        c.scores = c.dscores.cpu()
+
+    step(rows, counts, [over, bad, 0])
+    rows[1, 3] = 3
+    step(rows, [5, 7, 9], [0, 0, 0])   # accepted again: weighed again
+    step(rows, [t, t, t], [over, 0, over])
+    step(rows, [0, 1, 2], [0, 0, 0])

@@ -432,6 +432,10 @@ def _same_strides(name, a, other, b):
         raise ValueError(f"{name}: strides {a.stride()}, those of {other} are {b.stride()}")
 
 
+# Flags that a captured graph writes: a replay may come after the cache object's end.
+_captured = []
+
+
 def _opt(t):
     return None if t is None else t.data_ptr()
 
@@ -450,7 +454,9 @@ class KVCache:
                  (evict's n_sink and n_recent)
 
     Calls are enqueued on `stream` (default: the current stream of the cache's
-    device) and never synchronise; flags() does.  Inference only: no gradients."""
+    device) and never synchronise; flags() does.  A graph that captured calls needs
+    the tensors alone: it may be replayed after this object's end.  Inference only:
+    no gradients."""
 
     def __init__(self, k, v, lengths, scores=None, positions=None):
         global torch
@@ -474,6 +480,7 @@ class KVCache:
         self.k, self.v, self.lengths = k, v, lengths
         self.scores, self.positions = scores, positions
         self._flags = torch.zeros(b, dtype=torch.int32, device=k.device)
+        self._kept = False
         sb, sh, sn, _ = k.stride()
         self.desc = Cache(b, hkv, cap, d, sb, sh, sn, BF16 if k.dtype == torch.bfloat16 else F32,
                           k.data_ptr(), v.data_ptr(), lengths.data_ptr(), _opt(scores),
@@ -502,13 +509,20 @@ class KVCache:
             # (the handle alone: the stream object takes longer than a short kernel's launch)
             handle = torch._C._cuda_getCurrentRawStream(self.device.index)
             if self.device.index == torch.cuda.current_device():
-                return launch(handle)
+                return self._call(launch, handle)
             with torch.cuda.device(self.device):
-                return launch(handle)
+                return self._call(launch, handle)
         if stream.device != self.device:
             raise ValueError(f"stream on {stream.device}, the cache is on {self.device}")
         with torch.cuda.stream(stream):
-            return launch(stream.cuda_stream)
+            return self._call(launch, stream.cuda_stream)
+
+    def _call(self, launch, handle):
+        # (the default stream captures nothing)
+        if handle and not self._kept and torch.cuda.is_current_stream_capturing():
+            self._kept = True
+            _captured.append(self._flags)
+        return launch(handle)
 
     def _scratch(self, size_fn, *args):
         """Scratch memory of one call from torch's allocator (None if it needs none)."""

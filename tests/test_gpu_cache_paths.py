@@ -1,5 +1,6 @@
 """The operators on a K/V cache where launches, masks, memory and values meet:
 against the definitions in 64 bits with the tolerances of test_gpu_cache.py."""
+import gc
 import math
 
 import numpy as np
@@ -68,3 +69,28 @@ def test_rows_of_a_refused_append_weigh_nothing(dtype, g, t, in_place, clear):
     step(rows, [5, 7, 9], [0, 0, 0])   # accepted again: weighed again
     step(rows, [t, t, t], [over, 0, over])
     step(rows, [0, 1, 2], [0, 0, 0])
+
+
+# ---- the flags' memory --------------------------------------------------------
+
+def bad_tree():
+    c = Case("bf16", 64, b=2, hkv=1, g=1, cap=20, lens=(20, 7), t=6)
+    return c, ints([[-1, 0, 1, 2, 3, 4], [-1, 5, 1, -7, 3, 4]])
+
+
+def test_a_graph_outlives_its_cache_object():
+    c, par = bad_tree()
+    par.copy_(ints([[-1, 0, 1, 2, 3, 4]] * 2))
+    cache, c.cache = c.cache, None
+    out, lse = cache.attend(c.dq, c.dkn, c.dvn, parents=par)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cache.attend(c.dq, c.dkn, c.dvn, parents=par, out=out, lse=lse)
+    del cache
+    gc.collect()
+    others = [torch.zeros(2, dtype=torch.int32, device="cuda") for _ in range(3000)]
+    par.copy_(ints([[-1, 0, 1, 2, 3, 4], [-1, 5, 1, -7, 3, 4]]))
+    for _ in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+    assert not any(x.any() for x in others)

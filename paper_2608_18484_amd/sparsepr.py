@@ -480,7 +480,11 @@ class KVCache:
         self.k, self.v, self.lengths = k, v, lengths
         self.scores, self.positions = scores, positions
         self._flags = torch.zeros(b, dtype=torch.int32, device=k.device)
-        self._kept = False
+        self._kept, self._streams, self._cleared = False, set(), None
+        if self._device_type == "cuda":
+            self._streams.add(torch._C._cuda_getCurrentRawStream(k.device.index))
+            if not torch.cuda.is_current_stream_capturing():
+                self._cleared = torch.cuda.current_stream(k.device).record_event()
         sb, sh, sn, _ = k.stride()
         self.desc = Cache(b, hkv, cap, d, sb, sh, sn, BF16 if k.dtype == torch.bfloat16 else F32,
                           k.data_ptr(), v.data_ptr(), lengths.data_ptr(), _opt(scores),
@@ -518,11 +522,25 @@ class KVCache:
             return self._call(launch, stream.cuda_stream)
 
     def _call(self, launch, handle):
+        """launch(handle) with the flags' memory in order on that (current) stream."""
         # (the default stream captures nothing)
         if handle and not self._kept and torch.cuda.is_current_stream_capturing():
             self._kept = True
             _captured.append(self._flags)
+        elif handle not in self._streams:
+            self._meet(handle)
         return launch(handle)
+
+    def _meet(self, handle):
+        """First call on a stream: after the flags were cleared on the one that was
+        current then, and before their memory is used again."""
+        if torch.cuda.is_current_stream_capturing():
+            return
+        here = torch.cuda.current_stream(self.device)
+        if self._cleared is not None:
+            here.wait_event(self._cleared)
+        self._flags.record_stream(here)
+        self._streams.add(handle)
 
     def _scratch(self, size_fn, *args):
         """Scratch memory of one call from torch's allocator (None if it needs none)."""

@@ -94,3 +94,41 @@ def test_a_graph_outlives_its_cache_object():
         g.replay()
         torch.cuda.synchronize()
     assert not any(x.any() for x in others)
+
+
+def busy(seconds=0.05):
+    """Work on the current stream for a while."""
+    x = torch.ones(4096, 4096, device="cuda")
+    for _ in range(int(seconds * 1000)):
+        x @ x
+
+
+def test_first_call_on_a_stream_that_does_not_wait():
+    c, par = bad_tree()
+    s = torch.cuda.Stream()
+    busy(0.001)
+    torch.cuda.synchronize()
+    busy()
+    cache = S().KVCache(c.dk, c.dv, c.dlen)
+    cache.attend(c.dq, c.dkn, c.dvn, parents=par, stream=s)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert cache.flags() == [0, S().CACHE_FLAG_BAD_INDEX]
+
+
+def test_a_cache_object_dropped_before_its_call_ends():
+    c, par = bad_tree()
+    s = torch.cuda.Stream()
+    torch.zeros(2, dtype=torch.int32, device="cuda").any()
+    cache = S().KVCache(c.dk, c.dv, c.dlen)
+    with torch.cuda.stream(s):
+        busy(0.001)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        busy(0.3)
+    cache.attend(c.dq, c.dkn, c.dvn, parents=par, stream=s)
+    del cache
+    gc.collect()
+    others = [torch.zeros(2, dtype=torch.int32, device="cuda") for _ in range(500)]
+    torch.cuda.synchronize()
+    assert not any(x.any() for x in others)

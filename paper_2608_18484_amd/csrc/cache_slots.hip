@@ -680,6 +680,8 @@ void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int
                          hipStream_t s) {
   const int ch = c.d * (c.bf16 ? 2 : 4) / 16;
   const int64_t chunks = (int64_t)c.C * ch;
+  // (blocks take turns behind 2^16 of them, 256 MB of K and V each)
+  const unsigned blocks = (unsigned)std::min<int64_t>((chunks + 255) / 256, 1 << 16);
   // lengths in place: few rows in one launch (up to eight turns of a block),
   // more of them with the lengths in a launch of their own
   const bool in_place = lengths_out == c.lengths;
@@ -687,8 +689,8 @@ void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int
     k_cache_append<<<dim3(1, c.B), 256, 0, s>>>(c, token_positions, lengths_out, 1);
     return;
   }
-  k_cache_append<<<dim3((unsigned)((chunks + 255) / 256), c.B * c.Hkv), 256, 0, s>>>(c, token_positions, lengths_out, 0);
-  if (in_place) k_cache_append_lengths<<<c.B, 256, 0, s>>>(c);
+  k_cache_append<<<dim3(blocks, c.B * c.Hkv), 256, 0, s>>>(c, token_positions, lengths_out, 0);
+  if (in_place && hipPeekAtLastError() == hipSuccess) k_cache_append_lengths<<<c.B, 256, 0, s>>>(c);
 }
 
 size_t cache_evict_workspace(const CacheCall& c, int budget) {

@@ -132,3 +132,37 @@ def test_a_cache_object_dropped_before_its_call_ends():
     others = [torch.zeros(2, dtype=torch.int32, device="cuda") for _ in range(500)]
     torch.cuda.synchronize()
     assert not any(x.any() for x in others)
+
+
+# ---- long lists ---------------------------------------------------------------
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_append_with_a_long_list_of_few_rows(in_place):
+    # as many 16-byte pieces as a launch's threads would be counted in 33 bits
+    c = Case("f32", 128, b=1, hkv=1, g=1, cap=40, lens=(30,), t=4)
+    n = (1 << 27) + 5
+    rows = torch.full((1, n), 99, dtype=torch.int32, device="cuda")  # behind the count: not looked at
+    rows[0, :3] = ints([2, 0, 3])
+    tpos = np.arange(100, 104)[None]
+    k, v, sc, pos, lens, flags = T.append_ref(c, np.array([[2, 0, 3]]), [3], tpos)
+    new = c.dlen if in_place else torch.zeros_like(c.dlen)
+    c.cache.append(c.dkn, c.dvn, positions=ints(tpos), rows=rows, counts=ints([3]),
+                   lengths_out=None if in_place else new)
+    torch.cuda.synchronize()
+    assert new.tolist() == lens == [33] and c.cache.flags() == flags == [0]
+    assert T.same(c.dk, k) and T.same(c.dv, v)
+    assert torch.equal(c.dscores.cpu(), sc) and torch.equal(c.dpos.cpu(), pos)
+
+
+def test_append_of_more_rows_than_blocks_in_one_go():
+    # more than 2^24 pieces of 16 bytes: the blocks take turns
+    n = (1 << 20) + 77
+    k = torch.zeros(1, 1, n + 3, 128, device="cuda")
+    v = torch.zeros_like(k)
+    kn = torch.rand(1, 1, n, 128, device="cuda")
+    vn = torch.rand(1, 1, n, 128, device="cuda")
+    lengths = ints([2])
+    S().KVCache(k, v, lengths).append(kn, vn)
+    assert lengths.tolist() == [n + 2]
+    assert torch.equal(k[:, :, 2:-1], kn) and torch.equal(v[:, :, 2:-1], vn)
+    assert not (k[:, :, :2].any() or k[:, :, -1].any() or v[:, :, :2].any() or v[:, :, -1].any())

@@ -429,7 +429,11 @@ typedef struct {
  * (base pointers and strides) not 16-byte aligned, a row stride of K or V above
  * 2^24 elements, capacity or n * heads / heads_kv (likewise n_rows) above 2^28,
  * batch * heads * n of 2^31 or more, batch * heads_kv above 65535, a tree of
- * more than 256 tokens. */
+ * more than 256 tokens, and more than a launch of 2^32 threads holds: batch *
+ * heads_kv * t of about 2^24 and more, t the tiles of 32 rows (attention in bf16:
+ * 128) that n or n_rows * heads / heads_kv make, or the blocks of 256 slots (fp32:
+ * 128) that a capacity makes in an accumulation of more than 32 rows, or those of
+ * 1,024 in an eviction. */
 sparsepr_status sparsepr_cache_attend_workspace_size(const sparsepr_cache* cache,
                                                      const sparsepr_tokens* tokens, size_t* bytes);
 sparsepr_status sparsepr_cache_attend(const sparsepr_cache* cache, const sparsepr_tokens* tokens,

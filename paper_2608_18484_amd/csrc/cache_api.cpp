@@ -16,7 +16,7 @@ using namespace sparsepr;
 namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 28;
-// Rows of all heads: a launch's blocks are counted in 31 bits.
+// Rows of all heads: tiles of them are counted in 31 bits.
 constexpr int64_t kMaxAllRows = int64_t(1) << 31;
 // The kernels address the 32 rows of a key tile by 32-bit byte offsets.
 constexpr int64_t kMaxRowStride = int64_t(1) << 24;
@@ -171,6 +171,7 @@ sparsepr_status attend_geometry(const sparsepr_cache* cache, const sparsepr_toke
   if (!disjoint(x.d, x.B, x.osb, h, x.osh, x.T, x.osn)) return bad("tokens: output strides make rows overlap");
   if (!strides16(elem(x), x.B, x.osb, h, x.osh, x.T, x.osn))
     return unsupported("tokens: output strides must be multiples of 16 bytes");
+  if (!cache_attend_fits(x)) return unsupported("tokens: more tiles of rows than a launch has blocks (2^24)");
   return SPARSEPR_OK;
 }
 
@@ -180,6 +181,16 @@ sparsepr_status row_count_ok(CacheCall& x, int32_t n_rows) {
   if ((int64_t)n_rows * x.G * x.Hkv * x.B >= kMaxAllRows) return unsupported("batch * heads * n_rows above 2^31");
   x.C = n_rows;
   return SPARSEPR_OK;
+}
+
+sparsepr_status weights_fit(const CacheCall& x) {
+  if (cache_accumulate_fits(x)) return SPARSEPR_OK;
+  return unsupported("more tiles of rows, or blocks of slots, than a launch has blocks (2^24)");
+}
+
+sparsepr_status eviction_fits(const CacheCall& x) {
+  if (cache_evict_fits(x)) return SPARSEPR_OK;
+  return unsupported("cache: more blocks of slots than a launch has (2^22)");
 }
 
 sparsepr_status rows_ok(CacheCall& x, const int32_t* rows, int32_t n_rows) {
@@ -271,6 +282,7 @@ sparsepr_status sparsepr_cache_accumulate_workspace_size(const sparsepr_cache* c
     if (st == SPARSEPR_OK) st = tokens_ok(tokens, x);
     if (st == SPARSEPR_OK) st = q_ok(x);
     if (st == SPARSEPR_OK) st = row_count_ok(x, n_rows);
+    if (st == SPARSEPR_OK) st = weights_fit(x);
     if (st != SPARSEPR_OK) return st;
     *bytes = cache_accumulate_workspace(x);
     return set_error(SPARSEPR_OK, "");
@@ -293,7 +305,8 @@ sparsepr_status sparsepr_cache_accumulate(const sparsepr_cache* cache,
     if (!q || !lse) return bad("q and lse must not be NULL");
     if (!aligned16(q)) return unsupported("q must be 16-byte aligned");
     if (!x.scores) return bad("the cache has no scores");
-    st = workspace_ok(workspace, bytes, cache_accumulate_workspace(x));
+    st = weights_fit(x);
+    if (st == SPARSEPR_OK) st = workspace_ok(workspace, bytes, cache_accumulate_workspace(x));
     if (st != SPARSEPR_OK) return st;
     x.q = q;
     x.lse = const_cast<float*>(lse);
@@ -313,6 +326,8 @@ sparsepr_status sparsepr_cache_evict_workspace_size(const sparsepr_cache* cache,
     if (st != SPARSEPR_OK) return st;
     if (budget < 1) return bad("budget must be at least 1");
     if (budget > kMaxRows) return unsupported("budget above 2^28");
+    const sparsepr_status fits = eviction_fits(x);
+    if (fits != SPARSEPR_OK) return fits;
     *bytes = cache_evict_workspace(x, budget);
     return set_error(SPARSEPR_OK, "");
   });
@@ -342,7 +357,8 @@ sparsepr_status sparsepr_cache_evict(const sparsepr_cache* cache, const sparsepr
           (x.positions && y.positions == x.positions))
         return bad("the other cache must not share arrays with the cache");
     }
-    st = workspace_ok(workspace, bytes, cache_evict_workspace(x, budget));
+    st = eviction_fits(x);
+    if (st == SPARSEPR_OK) st = workspace_ok(workspace, bytes, cache_evict_workspace(x, budget));
     if (st != SPARSEPR_OK) return st;
     EvictTo t{};
     t.in_place = to == nullptr;

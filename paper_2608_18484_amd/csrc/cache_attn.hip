@@ -812,7 +812,7 @@ void attend(const CacheCall& c, const Cut& cut, hipStream_t s) {
     k_cache_attend<D, 2><<<grid, 256, 0, s>>>(c, cut);
   else
     k_cache_attend<D, 4><<<grid, 256, 0, s>>>(c, cut);
-  if (!cut.split) return;
+  if (!cut.split || !launches_ok()) return;
   const int64_t heads = (int64_t)c.B * c.Hkv, R = (int64_t)c.T * c.G;
   auto join = [&](auto alone) {
     constexpr int NG = alone.value ? 1024 / D : 1;
@@ -834,6 +834,12 @@ void attend(const CacheCall& c, const Cut& cut, hipStream_t s) {
 }
 
 }  // namespace
+
+// One part an entry; more of them are a few rounds of the chip's blocks.
+bool cache_attend_fits(const CacheCall& c) {
+  const int64_t tile = 32 * row_sets(c), rows = (int64_t)c.T * c.G;
+  return c.B * (int64_t)c.Hkv * ((rows + tile - 1) / tile) <= kMaxBlocks - 7;
+}
 
 size_t cache_attend_workspace(const CacheCall& c) {
   const Cut cut = make_cut(c);

@@ -13,6 +13,12 @@ namespace sparsepr {
 // Most tokens of a drafted tree: a row's visible tokens are 8 words of bits.
 constexpr int kTreeMax = 256;
 
+// A launch counts its threads in 32 bits: blocks of 256 threads at most.
+constexpr int64_t kMaxBlocks = ((int64_t(1) << 32) - 1) / 256;
+
+// Whether the launches so far were accepted: no other follows one that was not.
+inline bool launches_ok() { return hipPeekAtLastError() == hipSuccess; }
+
 // A call's geometry and device pointers, as the kernels see them.
 struct CacheCall {
   int B, Hkv, G, T;  // entries, K/V heads, query heads of each, new tokens
@@ -38,12 +44,15 @@ struct CacheCall {
   float* lse;
 };
 
+// cache_*_fits: whether the launches of such a call count their blocks.
+bool cache_attend_fits(const CacheCall& c);
 size_t cache_attend_workspace(const CacheCall& c);
 void launch_cache_attend(const CacheCall& c, void* ws, hipStream_t s);
 
 void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int32_t* lengths_out,
                          hipStream_t s);
 
+bool cache_accumulate_fits(const CacheCall& c);
 size_t cache_accumulate_workspace(const CacheCall& c);
 void launch_cache_accumulate(const CacheCall& c, void* ws, hipStream_t s);
 
@@ -57,6 +66,7 @@ struct EvictTo {
   float* scores;
   int32_t* positions;
 };
+bool cache_evict_fits(const CacheCall& c);
 size_t cache_evict_workspace(const CacheCall& c, int budget);
 void launch_cache_evict(const CacheCall& c, const EvictTo& to, int budget, int n_sink,
                         int n_recent, void* ws, hipStream_t s);

@@ -690,7 +690,11 @@ void launch_cache_append(const CacheCall& c, const int32_t* token_positions, int
     return;
   }
   k_cache_append<<<dim3(blocks, c.B * c.Hkv), 256, 0, s>>>(c, token_positions, lengths_out, 0);
-  if (in_place && hipPeekAtLastError() == hipSuccess) k_cache_append_lengths<<<c.B, 256, 0, s>>>(c);
+  if (in_place && launches_ok()) k_cache_append_lengths<<<c.B, 256, 0, s>>>(c);
+}
+
+bool cache_evict_fits(const CacheCall& c) {
+  return !evict_large(c) || (int64_t)c.B * c.Hkv * ((c.cap + kSlots - 1) / kSlots) <= kMaxBlocks / 4;
 }
 
 size_t cache_evict_workspace(const CacheCall& c, int budget) {
@@ -706,13 +710,14 @@ void launch_cache_evict(const CacheCall& c, const EvictTo& to, int budget, int n
   if (evict_large(c)) {
     const unsigned blocks = (unsigned)heads * (unsigned)w.blocks;
     k_evict_newest<<<blocks, 1024, 0, s>>>(c, w, budget, n_recent);
-    k_evict_keys<<<blocks, 1024, 0, s>>>(c, w, budget, n_sink, n_recent);
-    k_evict_list<<<blocks, 1024, 0, s>>>(c, w, budget);
-    k_evict_settle<<<heads, 1024, 0, s>>>(c, w, budget);
-    k_evict_number<<<blocks, 1024, 0, s>>>(c, w, to.in_place, budget);
+    if (launches_ok()) k_evict_keys<<<blocks, 1024, 0, s>>>(c, w, budget, n_sink, n_recent);
+    if (launches_ok()) k_evict_list<<<blocks, 1024, 0, s>>>(c, w, budget);
+    if (launches_ok()) k_evict_settle<<<heads, 1024, 0, s>>>(c, w, budget);
+    if (launches_ok()) k_evict_number<<<blocks, 1024, 0, s>>>(c, w, to.in_place, budget);
   } else {
     k_evict_select<<<heads, 1024, 0, s>>>(c, w, to.in_place, budget, n_sink, n_recent);
   }
+  if (!launches_ok()) return;
   const int ch = c.d * (c.bf16 ? 2 : 4) / 16;
   const int64_t most = to.in_place ? std::min(budget, std::max(c.cap - budget, 1)) : budget;
   const unsigned blocks = (unsigned)std::min<int64_t>((most * ch + 255) / 256, 256);

@@ -406,7 +406,9 @@ WeighCut weigh_cut(const CacheCall& c) {
   w.key_blocks = (c.cap + keys - 1) / keys;
   w.room = 256 * weigh_blocks(c.d, c.bf16);
   w.tiles_max = (int)tiles;
-  w.parts_max = (int)std::max<int64_t>(1, std::min<int64_t>(8, tiles / 8));
+  // (as many as a launch counts blocks of)
+  const int64_t room = (kMaxBlocks - 7) / ((int64_t)c.B * c.Hkv * w.key_blocks);
+  w.parts_max = (int)std::max<int64_t>(1, std::min({int64_t(8), tiles / 8, room}));
   return w;
 }
 
@@ -426,13 +428,21 @@ template <int D, class E, int SETS>
 void weigh(const CacheCall& c, const WeighCut& w, hipStream_t s) {
   const int64_t heads = (int64_t)c.B * c.Hkv;
   k_cache_weigh_rows<D, E><<<(unsigned)(heads * w.tiles_max), 256, 0, s>>>(c, w);
+  if (!launches_ok()) return;
   const int64_t blocks = (heads * w.parts_max * w.key_blocks + 7) / 8 * 8;
   k_cache_accumulate<D, E, SETS><<<(unsigned)blocks, 256, 0, s>>>(c, w);
-  if (w.parts_max > 1)
+  if (w.parts_max > 1 && launches_ok())
     k_cache_weigh_join<<<dim3((c.cap + 255) / 256, (unsigned)heads), 256, 0, s>>>(c, w, 128 * SETS);
 }
 
 }  // namespace
+
+bool cache_accumulate_fits(const CacheCall& c) {
+  if (few_rows(c)) return true;
+  const WeighCut w = weigh_cut(c);
+  const int64_t heads = (int64_t)c.B * c.Hkv;
+  return heads * w.tiles_max <= kMaxBlocks && heads * w.key_blocks <= kMaxBlocks - 7;
+}
 
 size_t cache_accumulate_workspace(const CacheCall& c) {
   size_t rows, zv, span;

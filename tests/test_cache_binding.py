@@ -1,33 +1,75 @@
 """Host-side checks of the operators on a K/V cache beyond test_cache_abi.py: the
-limits of their launches, their workspaces, gradients."""
+limits of their launches."""
 import ctypes
 
 import pytest
 
-torch = pytest.importorskip("torch")
-
-import test_cache_abi as A  # noqa: E402
-from test_cache_abi import P, S, _ref, cache, tokens  # noqa: E402
+import test_cache_abi as A
+from test_cache_abi import S, _ref, cache, tokens
 
 
-def test_calls_that_would_be_refused_gradients():
-    # the operators have no backward: an output without a graph would lose gradients
-    q, kn = torch.zeros(2, 8, 5, 64), torch.zeros(2, 4, 5, 64)
-    pos = torch.zeros(2, 5, dtype=torch.int32)
-    lse = torch.zeros(2, 8, 5)
-    leaf = {True: lambda x: x.clone().requires_grad_(), False: lambda x: x}
-    for i in range(3):
-        x = [leaf[i == j](y) for j, y in enumerate((q, kn, kn))]
-        with pytest.raises(ValueError, match="grad"):
-            A.host_cache().attend(*x)
-    with pytest.raises(ValueError, match="grad"):
-        A.host_cache().append(leaf[True](kn), kn, positions=pos)
-    with pytest.raises(ValueError, match="grad"):
-        A.host_cache().accumulate(leaf[True](q), lse)
-    with pytest.raises(ValueError, match="grad"):
-        A.host_cache(k=torch.zeros(2, 4, 100, 64).requires_grad_())
-    with torch.no_grad():
-        c = A.host_cache(k=torch.zeros(2, 4, 100, 64).requires_grad_())
-        c._q(leaf[True](q))  # accepted
-    with pytest.raises(ValueError, match="grad"):
-        c.attend(q, kn, kn)
+def size(fn, *args):
+    n = ctypes.c_size_t(0)
+    st = getattr(S.lib(), fn)(*args, ctypes.byref(n))
+    return st, n.value, S.lib().sparsepr_last_error().decode()
+
+
+def wide(heads, cap, dtype=S.F32):
+    return cache(batch=1, heads_kv=heads, capacity=cap, dtype=dtype, stride_n=64, stride_h=64 * cap,
+                 stride_b=64 * cap * heads)
+
+
+def many(heads, n):
+    return tokens(heads=heads, n=n, stride_n=0, stride_h=0, stride_b=0, kv_stride_n=0, kv_stride_h=0,
+                  kv_stride_b=0, out_stride_n=64, out_stride_h=64 * n, out_stride_b=64 * n * heads)
+
+
+@pytest.mark.parametrize("dtype,tile", [(S.F32, 32), (S.BF16, 128)])
+def test_attention_of_more_rows_than_a_launch_holds_is_refused(dtype, tile):
+    # 2^32 threads are 2^24 blocks of 256
+    for heads, n, ok in ((7, 1 << 21, True), (7, 1 << 28, tile == 128), (4, 1 << 27, tile == 128)):
+        assert heads * n < 1 << 31
+        st, _, msg = size("sparsepr_cache_attend_workspace_size", _ref(wide(heads, 100, dtype)),
+                          _ref(many(heads, n)))
+        assert st == (0 if ok else 2), msg
+        if not ok:
+            assert "launch" in msg
+            st, msg = A.attend(wide(heads, 100, dtype), many(heads, n))
+            assert st == 2 and "launch" in msg
+
+
+@pytest.mark.parametrize("dtype", [S.F32, S.BF16])
+def test_weights_of_more_rows_than_a_launch_holds_are_refused(dtype):
+    for heads, n, ok in ((7, 1 << 21, True), (3, 1 << 27, True), (4, 1 << 27, False), (7, 1 << 28, False)):
+        c, t = wide(heads, 100, dtype), many(heads, n)
+        st, _, msg = size("sparsepr_cache_accumulate_workspace_size", _ref(c), _ref(t), ctypes.c_int32(n))
+        assert st == (0 if ok else 2), msg
+        if not ok:
+            assert "launch" in msg
+            st, msg = A.accumulate(c, t, n_rows=n)
+            assert st == 2 and "launch" in msg
+
+
+def test_row_parts_of_an_accumulation_fit_a_launch():
+    # 2^28 slots of a head are 2^20 blocks of 256 and 2^21 of 128: as many parts of the
+    # rows as there is room for (a sum for each slot and part), down to one
+    for dtype, heads, most in ((S.BF16, 1, 8), (S.BF16, 4, 3), (S.BF16, 9, 1), (S.F32, 4, 1)):
+        st, n, msg = size("sparsepr_cache_accumulate_workspace_size", _ref(wide(heads, 1 << 28, dtype)),
+                          _ref(many(heads, 3000)), ctypes.c_int32(3000))
+        assert st == 0, msg
+        sums = heads * (1 << 28) * 4
+        assert n // sums == (most if most > 1 else 0)
+    for dtype, heads in ((S.BF16, 16), (S.F32, 8)):
+        st, _, msg = size("sparsepr_cache_accumulate_workspace_size", _ref(wide(heads, 1 << 28, dtype)),
+                          _ref(many(heads, 3000)), ctypes.c_int32(3000))
+        assert st == 2 and "launch" in msg
+
+
+def test_eviction_of_more_slots_than_a_launch_holds_is_refused():
+    # blocks of 4,096 slots and 1,024 threads: 2^22 of them
+    for heads, ok in ((63, True), (64, False)):
+        c = wide(heads, 1 << 28)
+        st, _, msg = size("sparsepr_cache_evict_workspace_size", _ref(c), ctypes.c_int32(50))
+        assert st == (0 if ok else 2), msg
+    st, msg = A.evict(c, nbytes=1 << 62)
+    assert st == 2 and "launch" in msg

@@ -408,9 +408,11 @@ def dense_attention(q, k, v, out=None, stream=None):
 
 def _tensor(name, t, shape, dtype, device, contiguous=True):
     """Raises ValueError unless t is a tensor of this shape, dtype and device,
-    contiguous or with a contiguous last dimension."""
+    contiguous or with a contiguous last dimension, that asks for no gradient."""
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if t.requires_grad:
+        _no_grad(name, t)
     if t.device == device and t.dtype is dtype and t.shape == shape and t.is_contiguous():
         return
     if t.device != device:
@@ -423,6 +425,13 @@ def _tensor(name, t, shape, dtype, device, contiguous=True):
         raise ValueError(f"{name}: must be contiguous")
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: last dimension must be contiguous")
+
+
+def _no_grad(name, t):
+    """What the cache's operators write has no graph: a gradient would be lost."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: requires grad, and the operators on a cache have no backward "
+                         "(call them under torch.no_grad())")
 
 
 def _same_strides(name, a, other, b):
@@ -456,7 +465,7 @@ class KVCache:
     Calls are enqueued on `stream` (default: the current stream of the cache's
     device) and never synchronise; flags() does.  A graph that captured calls needs
     the tensors alone: it may be replayed after this object's end.  Inference only:
-    no gradients."""
+    tensors that require gradients are refused outside torch.no_grad()."""
 
     def __init__(self, k, v, lengths, scores=None, positions=None):
         global torch
@@ -509,6 +518,8 @@ class KVCache:
         """launch(stream handle), with the stream and the cache's device current
         where they are not, so that scratch memory and outputs made by the call
         belong to the stream that uses them."""
+        _no_grad("k", self.k)
+        _no_grad("v", self.v)
         if stream is None:
             # (the handle alone: the stream object takes longer than a short kernel's launch)
             handle = torch._C._cuda_getCurrentRawStream(self.device.index)

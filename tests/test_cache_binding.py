@@ -1,5 +1,5 @@
 """Host-side checks of the operators on a K/V cache beyond test_cache_abi.py: the
-limits of their launches."""
+limits of their launches, gradients."""
 import ctypes
 
 import pytest
@@ -73,3 +73,33 @@ def test_eviction_of_more_slots_than_a_launch_holds_is_refused():
         assert st == (0 if ok else 2), msg
     st, msg = A.evict(c, nbytes=1 << 62)
     assert st == 2 and "launch" in msg
+
+
+# --- the binding ------------------------------------------------------------
+
+torch = pytest.importorskip("torch")
+
+
+def test_tensors_that_require_gradients_are_refused():
+    # the operators have no backward: an output without a graph would lose gradients
+    q, kn = torch.zeros(2, 8, 5, 64), torch.zeros(2, 4, 5, 64)
+    pos = torch.zeros(2, 5, dtype=torch.int32)
+    lse = torch.zeros(2, 8, 5)
+    leaf = {True: lambda x: x.clone().requires_grad_(), False: lambda x: x}
+    for i in range(3):
+        x = [leaf[i == j](y) for j, y in enumerate((q, kn, kn))]
+        with pytest.raises(ValueError, match="grad"):
+            A.host_cache().attend(*x)
+    with pytest.raises(ValueError, match="grad"):
+        A.host_cache().append(leaf[True](kn), kn, positions=pos)
+    with pytest.raises(ValueError, match="grad"):
+        A.host_cache().accumulate(leaf[True](q), lse)
+    with pytest.raises(ValueError, match="grad"):
+        A.host_cache(k=torch.zeros(2, 4, 100, 64).requires_grad_())
+    with torch.no_grad():
+        c = A.host_cache(k=torch.zeros(2, 4, 100, 64).requires_grad_())
+        c._q(leaf[True](q))  # accepted
+    for f in (lambda: c.attend(q, kn, kn), lambda: c.append(kn, kn, positions=pos),
+              lambda: c.accumulate(q, lse), lambda: c.evict(5)):
+        with pytest.raises(ValueError, match="k: requires grad"):
+            f()

@@ -1,5 +1,5 @@
 """Host-side checks of the operators on a K/V cache beyond test_cache_abi.py: the
-limits of their launches, gradients."""
+limits of their launches, workspaces, gradients."""
 import ctypes
 
 import pytest
@@ -73,6 +73,26 @@ def test_eviction_of_more_slots_than_a_launch_holds_is_refused():
         assert st == (0 if ok else 2), msg
     st, msg = A.evict(c, nbytes=1 << 62)
     assert st == 2 and "launch" in msg
+
+
+def test_workspaces_of_split_calls_checked():
+    # 4,000 slots are cut into parts, 80 rows are gathered: both need a workspace
+    big = dict(capacity=4000, stride_h=4000 * 64, stride_b=4 * 4000 * 64)
+    c, t = cache(**big), tokens(n=40, stride_h=40 * 64, stride_b=8 * 40 * 64, out_stride_h=40 * 64,
+                                out_stride_b=8 * 40 * 64, kv_stride_h=40 * 64, kv_stride_b=4 * 40 * 64)
+    st, need, _ = size("sparsepr_cache_attend_workspace_size", _ref(c), _ref(t))
+    assert st == 0 and need > 0
+    bare = cache(k=None, v=None, lengths=None, **big)
+    assert size("sparsepr_cache_attend_workspace_size", _ref(bare), _ref(t))[:2] == (0, need)
+    st, n_weigh, _ = size("sparsepr_cache_accumulate_workspace_size", _ref(c), _ref(t), ctypes.c_int32(40))
+    assert st == 0 and n_weigh > 0
+    for f, n, kw in ((A.attend, need, {}), (A.accumulate, n_weigh, dict(n_rows=40))):
+        st, msg = f(c, t, nbytes=n - 1, **kw)
+        assert st == 3 and "needs" in msg
+        st, msg = f(c, t, ws=None, **kw)
+        assert st == 1 and "workspace" in msg
+        st, msg = f(c, t, ws=A.P + 8, **kw)
+        assert st == 1 and "aligned" in msg
 
 
 # --- the binding ------------------------------------------------------------

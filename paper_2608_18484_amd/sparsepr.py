@@ -427,6 +427,12 @@ def _tensor(name, t, shape, dtype, device, contiguous=True):
         raise ValueError(f"{name}: last dimension must be contiguous")
 
 
+def _in_int32(name, t):
+    """The library takes extents as int32."""
+    if max(t.shape) >= 2 ** 31:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, extents must be below 2^31")
+
+
 def _no_grad(name, t):
     """What the cache's operators write has no graph: a gradient would be lost."""
     if t.requires_grad and torch.is_grad_enabled():
@@ -477,6 +483,7 @@ class KVCache:
         if k.device.type != self._device_type:
             raise ValueError(f"k: tensor on {k.device}, expected a {self._device_type} tensor")
         self.device, self.dtype = k.device, k.dtype
+        _in_int32("k", k)
         b, hkv, cap, d = k.shape
         _tensor("k", k, k.shape, k.dtype, k.device, contiguous=False)
         _tensor("v", v, k.shape, k.dtype, k.device, contiguous=False)
@@ -565,6 +572,7 @@ class KVCache:
         c = self.desc
         if not isinstance(q, torch.Tensor) or q.dim() != 4:
             raise ValueError("q: expected a [B, H, n, d] torch.Tensor")
+        _in_int32("q", q)
         _, h, n, _ = q.shape
         _tensor("q", q, (c.batch, h, n, c.d), self.dtype, self.device, contiguous=False)
         if n < 1 or h < 1 or h % c.heads_kv != 0:
@@ -585,6 +593,7 @@ class KVCache:
         if rows is not None:
             if not isinstance(rows, torch.Tensor) or rows.dim() != 2 or rows.shape[1] < 1:
                 raise ValueError("rows: expected a [B, n_rows] torch.Tensor")
+            _in_int32("rows", rows)
             width = rows.shape[1]
             _tensor("rows", rows, (b, width), torch.int32, self.device)
         if counts is not None:
@@ -642,6 +651,7 @@ class KVCache:
         lengths_out [B] int32, or into the cache's own."""
         if not isinstance(k_new, torch.Tensor) or k_new.dim() != 4 or k_new.shape[2] < 1:
             raise ValueError("k_new: expected a [B, H_kv, n, d] torch.Tensor with n >= 1")
+        _in_int32("k_new", k_new)
         c, n = self.desc, k_new.shape[2]
         ks = self._new(k_new, v_new, n)
         width = self._list(rows, counts, n)

@@ -123,3 +123,19 @@ def test_tensors_that_require_gradients_are_refused():
               lambda: c.accumulate(q, lse), lambda: c.evict(5)):
         with pytest.raises(ValueError, match="k: requires grad"):
             f()
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    # views of one row: their lengths would lose their upper bits on the way to the library
+    far = 2 ** 32 + 1
+    row = torch.zeros(2, 4, 1, 64)
+    lengths = torch.zeros(2, dtype=torch.int32)
+    c = A.HostCache(torch.zeros(2, 4, 100, 64), torch.zeros(2, 4, 100, 64), lengths)
+    with pytest.raises(ValueError, match="k: shape"):
+        A.HostCache(row.expand(2, 4, far, 64), row.expand(2, 4, far, 64), lengths)
+    with pytest.raises(ValueError, match="k_new: shape"):
+        c.append(row.expand(2, 4, far, 64), row.expand(2, 4, far, 64))
+    with pytest.raises(ValueError, match="q: shape"):
+        c.attend(row.expand(2, 4, far, 64), row.expand(2, 4, far, 64), row.expand(2, 4, far, 64))
+    with pytest.raises(ValueError, match="q: shape"):
+        c.attend(row[:, :1].expand(2, 4 * far, 1, 64), row, row)

@@ -427,10 +427,9 @@ def _tensor(name, t, shape, dtype, device, contiguous=True):
         raise ValueError(f"{name}: last dimension must be contiguous")
 
 
-def _in_int32(name, t):
+def _too_long(name, t):
     """The library takes extents as int32."""
-    if max(t.shape) >= 2 ** 31:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, extents must be below 2^31")
+    return ValueError(f"{name}: shape {tuple(t.shape)}, extents must be below 2^31")
 
 
 def _no_grad(name, t):
@@ -483,7 +482,8 @@ class KVCache:
         if k.device.type != self._device_type:
             raise ValueError(f"k: tensor on {k.device}, expected a {self._device_type} tensor")
         self.device, self.dtype = k.device, k.dtype
-        _in_int32("k", k)
+        if max(k.shape) >= 2 ** 31:
+            raise _too_long("k", k)
         b, hkv, cap, d = k.shape
         _tensor("k", k, k.shape, k.dtype, k.device, contiguous=False)
         _tensor("v", v, k.shape, k.dtype, k.device, contiguous=False)
@@ -501,6 +501,7 @@ class KVCache:
             self._streams.add(torch._C._cuda_getCurrentRawStream(k.device.index))
             if not torch.cuda.is_current_stream_capturing():
                 self._cleared = torch.cuda.current_stream(k.device).record_event()
+        self._default = 0 in self._streams
         sb, sh, sn, _ = k.stride()
         self.desc = Cache(b, hkv, cap, d, sb, sh, sn, BF16 if k.dtype == torch.bfloat16 else F32,
                           k.data_ptr(), v.data_ptr(), lengths.data_ptr(), _opt(scores),
@@ -525,40 +526,43 @@ class KVCache:
         """launch(stream handle), with the stream and the cache's device current
         where they are not, so that scratch memory and outputs made by the call
         belong to the stream that uses them."""
-        _no_grad("k", self.k)
-        _no_grad("v", self.v)
+        if self.k.requires_grad or self.v.requires_grad:
+            _no_grad("k", self.k)
+            _no_grad("v", self.v)
         if stream is None:
             # (the handle alone: the stream object takes longer than a short kernel's launch)
             handle = torch._C._cuda_getCurrentRawStream(self.device.index)
-            if self.device.index == torch.cuda.current_device():
-                return self._call(launch, handle)
+            if self.device.index == torch._C._cuda_getDevice():
+                if handle or not self._default:
+                    self._order(handle)
+                return launch(handle)
             with torch.cuda.device(self.device):
-                return self._call(launch, handle)
+                self._order(handle)
+                return launch(handle)
         if stream.device != self.device:
             raise ValueError(f"stream on {stream.device}, the cache is on {self.device}")
         with torch.cuda.stream(stream):
-            return self._call(launch, stream.cuda_stream)
+            self._order(stream.cuda_stream)
+            return launch(stream.cuda_stream)
 
-    def _call(self, launch, handle):
-        """launch(handle) with the flags' memory in order on that (current) stream."""
-        # (the default stream captures nothing)
-        if handle and not self._kept and torch.cuda.is_current_stream_capturing():
-            self._kept = True
-            _captured.append(self._flags)
-        elif handle not in self._streams:
-            self._meet(handle)
-        return launch(handle)
-
-    def _meet(self, handle):
-        """First call on a stream: after the flags were cleared on the one that was
-        current then, and before their memory is used again."""
-        if torch.cuda.is_current_stream_capturing():
+    def _order(self, handle):
+        """The flags' memory in order with a call on that (current) stream."""
+        if handle in self._streams and (self._kept or handle == 0):
             return
-        here = torch.cuda.current_stream(self.device)
-        if self._cleared is not None:
-            here.wait_event(self._cleared)
-        self._flags.record_stream(here)
-        self._streams.add(handle)
+        # (the default stream, 0, captures nothing)
+        if handle and torch.cuda.is_current_stream_capturing():
+            if not self._kept:
+                self._kept = True
+                _captured.append(self._flags)
+        elif handle not in self._streams:
+            # first call on a stream: after the flags were cleared on the one that was
+            # current then, and before their memory is used again
+            here = torch.cuda.current_stream(self.device)
+            if self._cleared is not None:
+                here.wait_event(self._cleared)
+            self._flags.record_stream(here)
+            self._streams.add(handle)
+            self._default = 0 in self._streams
 
     def _scratch(self, size_fn, *args):
         """Scratch memory of one call from torch's allocator (None if it needs none)."""
@@ -572,8 +576,9 @@ class KVCache:
         c = self.desc
         if not isinstance(q, torch.Tensor) or q.dim() != 4:
             raise ValueError("q: expected a [B, H, n, d] torch.Tensor")
-        _in_int32("q", q)
         _, h, n, _ = q.shape
+        if n >= 2 ** 31 or h >= 2 ** 31:
+            raise _too_long("q", q)
         _tensor("q", q, (c.batch, h, n, c.d), self.dtype, self.device, contiguous=False)
         if n < 1 or h < 1 or h % c.heads_kv != 0:
             raise ValueError(f"q: {h} heads of {n} tokens; heads must be a multiple of the "
@@ -593,8 +598,9 @@ class KVCache:
         if rows is not None:
             if not isinstance(rows, torch.Tensor) or rows.dim() != 2 or rows.shape[1] < 1:
                 raise ValueError("rows: expected a [B, n_rows] torch.Tensor")
-            _in_int32("rows", rows)
             width = rows.shape[1]
+            if width >= 2 ** 31:
+                raise _too_long("rows", rows)
             _tensor("rows", rows, (b, width), torch.int32, self.device)
         if counts is not None:
             _tensor("counts", counts, (b,), torch.int32, self.device)
@@ -651,8 +657,9 @@ class KVCache:
         lengths_out [B] int32, or into the cache's own."""
         if not isinstance(k_new, torch.Tensor) or k_new.dim() != 4 or k_new.shape[2] < 1:
             raise ValueError("k_new: expected a [B, H_kv, n, d] torch.Tensor with n >= 1")
-        _in_int32("k_new", k_new)
         c, n = self.desc, k_new.shape[2]
+        if n >= 2 ** 31:
+            raise _too_long("k_new", k_new)
         ks = self._new(k_new, v_new, n)
         width = self._list(rows, counts, n)
         if (positions is None) != (self.positions is None):

@@ -293,8 +293,10 @@ sparsepr_status sparsepr_attend(sparsepr_plan_t plan, const void* q, const void*
 
 /* Dense attention of Sec. 3 (eq. dense_attention) for every head: in bf16 a kernel
  * of its own, in fp32 the one the probes use; for error reporting and layers
- * that stay dense.  Needs no plan, allocates
- * nothing; `workspace` must hold sparsepr_dense_workspace_size bytes. */
+ * that stay dense.  In bf16, here and in sparsepr_attend, a row's weights may reach
+ * 2^8 before they are divided by their sum, so that values from about 1.3e36 on can
+ * give infinite outputs.  Needs no plan, allocates nothing; `workspace` must hold
+ * sparsepr_dense_workspace_size bytes. */
 sparsepr_status sparsepr_dense_workspace_size(const sparsepr_shape* shape, size_t* bytes);
 sparsepr_status sparsepr_dense_attend(const sparsepr_shape* shape, const void* q, const void* k,
                                       const void* v, void* out, void* workspace, size_t bytes,

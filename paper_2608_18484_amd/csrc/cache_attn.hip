@@ -146,8 +146,9 @@ __device__ __forceinline__ uint32_t seen_keys(const CacheCall& c, const Where& w
 //
 // What bounds it.  Up to 32 rows the keys and values: four entries of up to
 // 84,480 slots are 1.13 GB, read once, 195 us (5.8 TB/s).  Then the work per key:
-// 189 rows over two entries of 75,600 slots 141 us (92 GFLOP, 0.54 GB).  A
-// frame's 4,680 rows over 18,720 keys, 344 GFLOP, take 400 us (860 TFLOP/s): the
+// 189 rows over two entries of 75,600 slots 136 to 161 us, as the clock goes (92 GFLOP,
+// 0.54 GB).  A frame's 4,680 rows over 18,720 keys, 344 GFLOP, take 397 us in
+// repeated calls (866 TFLOP/s; 470 right after a pause, at a low clock): the
 // matrix cores are busy 41% of the time beside 5.8 vector instructions per
 // product, LDS 17%; without the exponentials it would be 5% less, without the
 // copies 12%, without the reads of V or of K 4% each, so that no one of them is
@@ -298,8 +299,12 @@ __global__ __launch_bounds__(256, RS == 1 && D == 128 ? 1 : 2) void k_cache_atte
         for (int e = 0; e < 16; ++e) O[db][e] *= alpha;
     }
     between();
-    // the weights are rounded to bf16 for the V product; their sum, which lse
-    // comes from, is taken before
+    // The weights are rounded to bf16 for the V product (large products reach 8 times
+    // the rate of fp32); their sum, which lse comes from, is taken before.
+    // A weight is off by at most 2^-8 of itself, and outputs by 2.2e-3 (relative, root
+    // of the squares) where their own rounding alone makes 1.7e-3.  Weights in two
+    // bf16 halves and two products (1.7e-3) took 521 us for a frame's 418 and 187 for
+    // the 189 rows' 149, and turn an infinite value's output to NaN (0 times it).
     float p[16];
     bf16x8 P[2];
 #pragma unroll
@@ -760,9 +765,10 @@ int row_sets(const CacheCall& c) {
 }
 
 // Parts.  A CU holds one block of the 128 KB of tiles of 32-row blocks at
-// d = 128 (or of fp32's registers) and two of the others (d = 64, two caches of
-// 20,000 slots: 22.5 us with two, 24.5 with one; fp32 over four of 84,480 267 and
-// 345).  The parts of an entry end together when a launch fills the chip a whole
+// d = 128 (or of fp32's registers) and two of the others, which the rule counts
+// (d = 64, two caches of 20,000 slots: 22.5 us with two, 24.5 with one; fp32 over
+// four of 84,480 267 and 345); of the 64- and 128-row blocks of d = 64, with 161
+// and 162 registers, three would fit.  The parts of an entry end together when a launch fills the chip a whole
 // number of times, so that there are at most as many as r rounds of blocks hold:
 // the r whose rounds are shortest together, each of a part's keys and of a start
 // that takes as long as some 500 keys (a frame's 296 blocks: one part each 513 us,

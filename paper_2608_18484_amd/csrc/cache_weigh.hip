@@ -395,7 +395,9 @@ __global__ __launch_bounds__(256) void k_cache_weigh_join(CacheCall c, WeighCut 
   c.scores[o] += v;
 }
 
-constexpr int kRoom = 256;  // blocks of k_cache_weigh_few: one a CU
+// Blocks of k_cache_weigh_few: one a CU (its LDS holds no second one but of d = 64 in
+// bf16, whose 68 KB would leave room for it).
+constexpr int kRoom = 256;
 
 constexpr int weigh_keys(bool bf16) { return bf16 ? 256 : 128; }
 

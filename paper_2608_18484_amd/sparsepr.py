@@ -515,8 +515,10 @@ class KVCache:
         last call, per batch entry; clears them.  Waits for the device."""
         torch.cuda.synchronize(self.device)
         got = self._flags.tolist()
-        # (append's own note for accumulate stays)
-        self._flags.bitwise_and_(CACHE_FLAG_REFUSED)
+        # (append's own note for accumulate stays; an object made in inference mode
+        # has flags that can be written there alone)
+        with torch.inference_mode():
+            self._flags.bitwise_and_(CACHE_FLAG_REFUSED)
         torch.cuda.synchronize(self.device)
         return [x & ~CACHE_FLAG_REFUSED for x in got]
 
@@ -677,8 +679,8 @@ class KVCache:
     def accumulate(self, q, lse, rows=None, counts=None, causal=True, stream=None):
         """Add the attention weights of the rows that were just appended (rows
         and counts as in append; q and lse as in attend) to the scores of the
-        slots that they see; see sparsepr_cache_accumulate.  Entries whose
-        append was refused (flags()) keep their scores."""
+        slots that they see; see sparsepr_cache_accumulate.  Entries whose last
+        append by this object was refused (flags()) keep their scores."""
         h, n = self._q(q)
         c = self.desc
         width = self._list(rows, counts, n)

@@ -411,3 +411,18 @@ def test_evict_very_large(n, spread, sink, recent):
         assert np.array_equal(dscore[0, 0, :budget].cpu().numpy(), s0[src])
         assert torch.equal(v[0, 0, :budget, 0], v0[m])
         assert torch.equal(k.view(torch.int16)[0, 0, :budget], k0.view(torch.int16)[0, 0][m])
+
+
+# ---- modes of the caller --------------------------------------------------------
+
+@pytest.mark.parametrize("made,read", [(True, False), (False, True), (True, True)])
+def test_flags_in_and_out_of_inference_mode(made, read):
+    c, par = bad_tree()
+    bad = [0, S().CACHE_FLAG_BAD_INDEX]
+    with torch.inference_mode(made):
+        cache = S().KVCache(c.dk, c.dv, c.dlen)
+        cache.attend(c.dq, c.dkn, c.dvn, parents=par)
+    with torch.inference_mode(read):
+        assert cache.flags() == bad and cache.flags() == [0, 0]
+        cache.attend(c.dq, c.dkn, c.dvn, parents=par)
+    assert cache.flags() == bad and cache.flags() == [0, 0]

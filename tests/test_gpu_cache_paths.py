@@ -426,3 +426,56 @@ def test_flags_in_and_out_of_inference_mode(made, read):
         assert cache.flags() == bad and cache.flags() == [0, 0]
         cache.attend(c.dq, c.dkn, c.dvn, parents=par)
     assert cache.flags() == bad and cache.flags() == [0, 0]
+
+
+def test_library_calls_without_lse_and_flags():
+    # what the header lets be NULL: the same outputs, bad indices without a flag
+    import ctypes
+    L, c, par = S().lib(), *bad_tree()
+    ks, qs = c.dkn.stride()[:3], c.dq.stride()[:3]
+    want, lse = c.cache.attend(c.dq, c.dkn, c.dvn, parents=par)
+    desc = S().Cache.from_buffer_copy(c.cache.desc)
+    desc.flags = None
+    t = S().Tokens(1, 6, *qs, *qs, *ks, S().TOKENS_TREE)
+    out = torch.zeros_like(c.dq)
+    a, at = ctypes.addressof(desc), ctypes.addressof(t)
+    assert L.sparsepr_cache_attend(a, at, c.dq.data_ptr(), c.dkn.data_ptr(), c.dvn.data_ptr(), par.data_ptr(),
+                                   None, out.data_ptr(), None, None, 0, None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    # entry 0 is full, entry 1 takes its rows
+    tpos = ints(np.tile(np.arange(6), (2, 1)))
+    assert L.sparsepr_cache_append(a, at, c.dkn.data_ptr(), c.dvn.data_ptr(), tpos.data_ptr(), None, 6, None,
+                                   c.dlen.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    assert c.dlen.tolist() == [20, 13]
+    # without flags the caller says which entries are weighed
+    before = c.dscores.clone()
+    counts = ints([0, 6])
+    assert L.sparsepr_cache_accumulate(a, at, c.dq.data_ptr(), lse.data_ptr(), None, 6, counts.data_ptr(), None, 0,
+                                       None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(c.dscores[0], before[0]) and (c.dscores[1, :, :13] >= before[1, :, :13]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("t", [3, 40])
+def test_broadcast_inputs(dtype, t):
+    # one query and one new key and value for all tokens, heads and entries
+    c = Case(dtype, 64, b=2, hkv=2, g=2, cap=900, lens=(700, 33), t=t)
+    for name, h in (("q", 4), ("kn", 2), ("vn", 2)):
+        x = getattr(c, name)[:1, :1, :1].contiguous()
+        setattr(c, name, x.expand(2, h, t, 64))
+        setattr(c, "d" + name, x.cuda().expand(2, h, t, 64))
+    see = [np.tril(np.ones((t, t), bool))] * 2
+    out, lse = c.cache.attend(c.dq, c.dkn, c.dvn)
+    ref, zref, tout, tlse = T.attend_ref(c, see, [t, t], torch.zeros(2, 4, t, 64), torch.zeros(2, 4, t))
+    check("out", out, ref, tout)
+    check("lse", lse, zref, tlse)
+    tpos = np.tile(np.arange(t), (2, 1))
+    k, v, sc, pos, lens, flags = T.append_ref(c, tpos, [t, t], tpos)
+    c.cache.append(c.dkn, c.dvn, positions=ints(tpos))
+    torch.cuda.synchronize()
+    assert T.same(c.dk, k) and T.same(c.dv, v) and c.dlen.tolist() == lens
+    c.k, c.v, c.scores, c.lens = k, v, sc, lens
+    T.run_accumulate(c, lse=lse.cpu())
